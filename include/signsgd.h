@@ -31,7 +31,8 @@
  *              with sign(m_w).
  *
  * MEMORY      Every data pointer (g, m, x, packed, voted) is DEVICE memory,
- *             owned by the caller and 16-byte aligned.  A buffer that a call
+ *             owned by the caller and 16-byte aligned (where a call asks for
+ *             less, it says so).  A buffer that a call
  *             writes (m, x, packed, voted, sums, ...) may not share a byte with
  *             any other buffer of that call: SS_ERR_ARG, nothing launched.
  *             Buffers that are only read may coincide.  Arrays OF pointers
@@ -332,6 +333,115 @@ int ss_density(const float *v, size_t d, double *out, void *workspace, void *hip
  */
 #define SS_DENSITY_STATIC_MAX_D ((size_t)1 << 36)
 int ss_density_static(const float *v, size_t d, double *out, void *hip_stream);
+
+/* ---- gradients on their way into a step: global norm and clipping over many tensors ----
+ *
+ * A model's gradients are many tensors of two types; a step reads one vector per
+ * worker.  Signum sees a gradient only through its momentum's sign, so that a single
+ * outsized one decides the direction for 1/(1 - beta) steps: it is clipped before.
+ *   g    host array of n device pointers, aligned to their element and no more (views
+ *        into a larger buffer); an entry may be NULL where its length is 0
+ *   gdt  host array of n element types, which may differ
+ *   len  host array of n lengths; n and single lengths may be 0
+ * Tensors that are only read may coincide or overlap.
+ */
+
+/*
+ * norm <- sqrt( sum over all tensors and elements of g^2 ), rounded to fp32 once.
+ * Squares are exact in fp64 and added in fp64, in an order that depends on the
+ * lengths, types and the addresses modulo 16 alone: the same bits on every run.  Infinities and NaN
+ * follow the formula.  The norm of nothing is 0.
+ *   norm       out  one fp32 in DEVICE memory, 16-byte aligned
+ *   workspace  i/o  ss_grad_norm_workspace_bytes() bytes of DEVICE memory, under the same
+ *                   terms as that of ss_density
+ * One launch for every SS_GRAD_TENSORS_PER_LAUNCH tensors.
+ */
+#define SS_GRAD_TENSORS_PER_LAUNCH 176
+size_t ss_grad_norm_workspace_bytes(void);
+int ss_grad_norm(const void *const *g, const ss_dtype *gdt, const size_t *len, size_t n,
+                 float *norm, void *workspace, void *hip_stream);
+
+/*
+ * out_t <- c g_t with c = min(1, max_norm / (norm + 1e-6)) evaluated in fp32, each
+ * element fl(c * g) rounded to the type of out_t.  c is NaN where norm is.
+ *   norm      in   one fp32 in DEVICE memory: ss_grad_norm's, or a norm over more than
+ *                  these tensors (workers that hold parts of a model combine theirs)
+ *   max_norm       finite and >= 0, else SS_ERR_ARG
+ *   out       out  host array of n device pointers, aligned to their element, of len[t]
+ *                  elements of odt[t] each.  out[t] == g[t] with the same type clips in place;
+ *                  apart from that nothing that is written may share a byte with
+ *                  anything else of the call.  Parts of one vector: the gradients as a step
+ *                  reads them.
+ */
+int ss_grad_clip(const void *const *g, const ss_dtype *gdt, const size_t *len, size_t n,
+                 const float *norm, float max_norm, void *const *out, const ss_dtype *odt,
+                 void *hip_stream);
+
+/* ---- matrices in microscaled 4-bit floating point (MX4) ----
+ *
+ * The linear layers that gradients come from, on operands of 4.25 bits an element
+ * (OCP Microscaling: E2M1 elements, one E8M0 scale for 32 of them).
+ *   value   code * 2^(byte - 127); code magnitudes 0 0.5 1 1.5 2 3 4 6 for 0..7, bit 3 the
+ *           sign; byte 255: all 32 are NaN
+ *   layout  of a rows x cols matrix, blocks of 32 along the columns; P = ss_mx4_padded(cols)
+ *           data    rows x P/2 bytes, row-major: column 2j in the low half of byte j
+ *           scales  (P/128) x rows x 4 bytes: the four bytes of columns 128k .. 128k + 127 of a row
+ *                   side by side, the rows' after one another
+ *           Columns from cols to P hold code 0; a product reads them.  What this library
+ *           writes has byte 127 for blocks without any column.
+ * data and scales are 16-byte aligned device memory.  Plain matrices are row-major with a
+ * row every `ld` elements (ld >= cols) and need no more than their element's alignment.
+ * Neither rows nor columns may exceed SS_MX4_MAX_DIM, nor the elements of a plain matrix
+ * SS_MX4_MAX_ELEMENTS (else SS_ERR_ARG).
+ */
+#define SS_MX4_MAX_DIM ((size_t)1 << 27)
+#define SS_MX4_MAX_ELEMENTS ((size_t)1 << 34)
+size_t ss_mx4_padded(size_t cols);
+size_t ss_mx4_data_bytes(size_t rows, size_t cols);
+size_t ss_mx4_scale_bytes(size_t rows, size_t cols);
+
+/*
+ * x in MX4.  Per block of 32: amax = max |x|, scale 2^s with s = floor(log2(amax)) - 2
+ * (at least -127; 1 where amax is 0), each element x 2^-s rounded to the nearest code, ties to
+ * the even one, beyond 6 to 6.  A block that holds an infinity or a NaN is NaN.
+ *   x                   in   rows x cols
+ *   data, scales        out  x itself, blocks along its rows; both NULL: not wanted
+ *   data_t, scales_t    out  the transpose of x, cols x rows, blocks along its rows (down
+ *                            the columns of x); both NULL: not wanted
+ * Products sum over the blocked axis: y = x w^T takes x and w, dx = dy w takes dy and the transpose of w,
+ * dw = dy^T x the transposes of dy and x.  One pass over x gives both forms.
+ */
+int ss_mx4_quantize(const void *x, ss_dtype xdt, size_t rows, size_t cols, size_t ld,
+                    uint8_t *data, uint8_t *scales, uint8_t *data_t, uint8_t *scales_t,
+                    void *hip_stream);
+
+/* out (rows x cols, a row every ld elements) <- the values, exact in either type (a NaN block: NaN) */
+int ss_mx4_dequantize(const uint8_t *data, const uint8_t *scales, size_t rows, size_t cols,
+                      void *out, ss_dtype odt, size_t ld, void *hip_stream);
+
+/*
+ * out (M x N, a row every ld elements) <- a b^T, a of M x K and b of N x K in MX4.  Products are
+ * exact, sums in fp32, rounded once to the type of out.  K = 0 gives zeros.
+ *   scratch  work  ss_mx4_matmul_scratch_bytes(M, N, K) bytes of device memory, 16-byte aligned,
+ *                  contents immaterial before and after; untouched by others until the
+ *                  enqueued work has run.  NULL or smaller: one launch, which takes longer where that
+ *                  size is not 0 (small outputs with a long K).
+ * The order of the sums depends on M, N, K and on whether scratch is given.
+ */
+size_t ss_mx4_matmul_scratch_bytes(size_t M, size_t N, size_t K);
+int ss_mx4_matmul(const uint8_t *a_data, const uint8_t *a_scales, const uint8_t *b_data,
+                  const uint8_t *b_scales, size_t M, size_t N, size_t K, void *out,
+                  ss_dtype odt, size_t ld, void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/*
+ * out (T x N) <- x w^T for the few rows of an answering model: x of T x K (T at most
+ * SS_MX4_LINEAR_MAX_ROWS, else SS_ERR_ARG) is quantised on the way as ss_mx4_quantize does it,
+ * w of N x K is in MX4.  No memory for x in MX4 is needed; one launch (per 134 million rows of w).
+ */
+#define SS_MX4_LINEAR_MAX_ROWS 16
+int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8_t *w_data,
+                  const uint8_t *w_scales, size_t N, size_t K, void *out, ss_dtype odt,
+                  size_t ldo, void *hip_stream);
 
 /* the hipError_t (as int) behind this thread's most recent SS_ERR_HIP; 0 if none */
 int ss_last_hip_error(void);

@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     signum_vote_step_ex, stream_copy, sum_apply, vote_sum, warmup_length,
     density, density_static, new_density_workspace, welford_sigma, welford_update,
     quorum_vote, signum_pack_ternary, signum_vote_step_ternary, ternary_apply,
+    grad_clip, grad_norm, new_grad_norm_workspace,
+    Mx4, mx4_dequantize, mx4_linear, mx4_matmul, mx4_quantize, new_mx4,
 )

@@ -4,6 +4,7 @@ module _marshal (csrc/marshal.cpp); load_library() is the plain ctypes handle of
 libsignsgd.so for callers with raw pointers."""
 import ctypes
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -78,6 +79,24 @@ def load_library():
         L.ss_quorum_vote.argtypes = [vp, vp, i32, i32, vp, vp, sz, vp]
         L.ss_ternary_apply.argtypes = [vp, vp, vp, f32, sz, vp]
         L.ss_signum_vote_step_ternary.argtypes = [vp, i32, vp, i32, f32, f32, i32, f32, vp, vp, vp, sz, vp]
+        L.ss_grad_norm_workspace_bytes.restype = sz
+        L.ss_grad_norm_workspace_bytes.argtypes = []
+        L.ss_grad_norm.argtypes = [vp, vp, vp, sz, vp, vp, vp]
+        L.ss_grad_clip.argtypes = [vp, vp, vp, sz, vp, f32, vp, vp, vp]
+        L.ss_mx4_padded.restype = sz
+        L.ss_mx4_padded.argtypes = [sz]
+        for name in ("ss_mx4_data_bytes", "ss_mx4_scale_bytes"):
+            getattr(L, name).restype = sz
+            getattr(L, name).argtypes = [sz, sz]
+        L.ss_mx4_quantize.argtypes = [vp, i32, sz, sz, sz, vp, vp, vp, vp, vp]
+        L.ss_mx4_dequantize.argtypes = [vp, vp, sz, sz, vp, i32, sz, vp]
+        L.ss_mx4_matmul_scratch_bytes.restype = sz
+        L.ss_mx4_matmul_scratch_bytes.argtypes = [sz, sz, sz]
+        L.ss_mx4_matmul.argtypes = [vp, vp, vp, vp, sz, sz, sz, vp, i32, sz, vp, sz, vp]
+        L.ss_mx4_linear.argtypes = [vp, i32, sz, sz, vp, vp, sz, sz, vp, i32, sz, vp]
+        for name in ("ss_grad_norm", "ss_grad_clip", "ss_mx4_quantize", "ss_mx4_dequantize", "ss_mx4_matmul",
+                     "ss_mx4_linear"):
+            getattr(L, name).restype = i32
         for name in ("ss_signum_pack_ternary", "ss_quorum_vote", "ss_ternary_apply",
                      "ss_signum_vote_step_ternary"):
             getattr(L, name).restype = i32
@@ -253,3 +272,71 @@ def signum_vote_step_ternary(g, m, beta, tau, quorum, delta, x, voted_neg, voted
     (borrows memory as signum_vote_step does)"""
     _check("ss_signum_vote_step_ternary", (_marshal or _native()).signum_vote_step_ternary(
         g, m, beta, tau, quorum, delta, x, voted_neg, voted_zero, d, stream))
+
+
+# ---- gradients on their way into a step ----
+
+def new_grad_norm_workspace(device="cuda"):
+    """zero-filled workspace for ss_grad_norm (ss_grad_norm_workspace_bytes() bytes)"""
+    return torch.zeros(load_library().ss_grad_norm_workspace_bytes() // 8, dtype=torch.int64, device=device)
+
+
+def grad_norm(g, norm, workspace, stream=None):
+    """ss_grad_norm: norm (one float32 on the device) <- the 2-norm over all gradients in the sequence g, which may differ in
+    dtype (float32, bfloat16), shape and memory order and start at any element of a buffer.
+    workspace: new_grad_norm_workspace(), kept by the caller; two calls that may overlap in time need two."""
+    _check("ss_grad_norm", (_marshal or _native()).grad_norm(g, norm, workspace, stream))
+    return norm
+
+
+def grad_clip(g, norm, max_norm, out=None, stream=None):
+    """ss_grad_clip: out[t] <- g[t] * min(1, max_norm / (norm + 1e-6)) for every gradient; out None: in place.
+    out: as many tensors as g, of the same numbers of elements, float32 or bfloat16; the parts of one vector
+    (flat.split(lengths)) make it the gradient that a step takes.  norm: a float32 tensor on the device."""
+    _check("ss_grad_clip", (_marshal or _native()).grad_clip(g, norm, max_norm, out, stream))
+    return g if out is None else out
+
+
+# ---- matrices in microscaled 4-bit floating point ----
+
+class Mx4(NamedTuple):
+    """A rows x cols matrix in MX4, blocks of 32 along the columns (layout: include/signsgd.h).  With P = cols rounded up to
+    a multiple of 128: data has rows x P/2 bytes, column 2j in the low half of byte j; scales has P/128 x rows x 4."""
+    data: torch.Tensor
+    scales: torch.Tensor
+    rows: int
+    cols: int
+
+
+def new_mx4(rows, cols, device="cuda"):
+    """uninitialised Mx4 for rows x cols"""
+    p = load_library().ss_mx4_padded(cols)
+    return Mx4(torch.empty(rows, p // 2, dtype=torch.uint8, device=device),
+               torch.empty(p // 128, rows, 4, dtype=torch.uint8, device=device), rows, cols)
+
+
+def mx4_quantize(x, q=None, qt=None, stream=None):
+    """ss_mx4_quantize: q <- x in MX4, blocks along its rows; qt <- the transpose of x, blocks down the columns of x.
+    x: rows x cols, float32 or bfloat16, elements of a row side by side; q: new_mx4(rows, cols); qt: new_mx4(cols, rows);
+    either may be None."""
+    _check("ss_mx4_quantize", (_marshal or _native()).mx4_quantize(x, q, qt, stream))
+
+
+def mx4_dequantize(q, out, stream=None):
+    """ss_mx4_dequantize: out (q.rows x q.cols, float32 or bfloat16) <- the values that q stands for"""
+    _check("ss_mx4_dequantize", (_marshal or _native()).mx4_dequantize(q, out, stream))
+    return out
+
+
+def mx4_matmul(a, b, out, stream=None):
+    """ss_mx4_matmul: out (a.rows x b.rows, float32 or bfloat16) <- a b^T, sums in float32.  The passes of a layer
+    y = x w^T: y from x and w, dx from dy and the transpose of w, dw from the transposes of dy and x.
+    Borrows memory as signum_vote_step does where the output is small and the sums are long."""
+    _check("ss_mx4_matmul", (_marshal or _native()).mx4_matmul(a, b, out, stream))
+    return out
+
+
+def mx4_linear(x, w, out, stream=None):
+    """ss_mx4_linear: out <- x w^T for up to 16 rows of x (float32 or bfloat16), which is quantised on the way"""
+    _check("ss_mx4_linear", (_marshal or _native()).mx4_linear(x, w, out, stream))
+    return out

@@ -176,6 +176,30 @@ __device__ __forceinline__ uint32_t combine4(uint32_t byte, int lane) {
     return v;
 }
 
+// another lane's value, zero in the rows (of 16 lanes) that ROWS leaves out
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ double lane_move(double v) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, v);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+
+// sum over each eight lanes, in all of them
+__device__ __forceinline__ double sum8(double s) {
+    s += lane_move<0xB1 /* quad_perm [1,0,3,2] */>(s);
+    s += lane_move<0x4E /* quad_perm [2,3,0,1] */>(s);
+    return s + lane_move<0x141 /* row_half_mirror */>(s);
+}
+
+// sum over the wave, in lane 63
+__device__ __forceinline__ double sum_wave(double s) {
+    s = sum8(s);
+    s += lane_move<0x140 /* row_mirror */>(s);
+    s += lane_move<0x142 /* row_bcast:15 */, 0xA>(s);
+    return s + lane_move<0x143 /* row_bcast:31 */, 0xC>(s);
+}
+
 // Reserves HOLD_KB kilobytes of LDS in the kernel that calls it and never uses them: the only
 // effect is that fewer blocks fit into a compute unit's LDS, i.e. a cap on the traffic a unit
 // keeps in flight (see step_kernels.hpp for why that matters).  `never` must be false at run

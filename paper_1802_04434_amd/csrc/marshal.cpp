@@ -18,6 +18,7 @@
 #include <cstring>
 #include <exception>
 #include <stdexcept>
+#include <vector>
 
 #include "../../include/signsgd.h"
 
@@ -529,12 +530,198 @@ PyObject *signum_vote_step_ternary(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- lists of gradients ----
+
+// n tensors of either gradient type, as the library takes them
+struct Gradients {
+    std::vector<const at::Tensor *> t;
+    std::vector<void *> p;
+    std::vector<ss_dtype> dtype;
+    std::vector<size_t> len;
+    // what holds the tensors until the call is over, should they exist for it alone (rows of a stacked tensor)
+    struct Held {
+        PyObject *o;
+        ~Held() { Py_XDECREF(o); }
+    } held;
+
+    Gradients(const Gradients &) = delete;
+    Gradients(PyObject *seq, const char *name) : held{PySequence_Fast(seq, "a sequence of tensors is wanted")} {
+        PyObject *fast = held.o;
+        if (!fast) throw PyRaised();
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(fast);
+        PyObject **items = PySequence_Fast_ITEMS(fast);
+        t.reserve(n), p.reserve(n), dtype.reserve(n), len.reserve(n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            const at::Tensor &g = tensor(items[i], name, (int)i);
+            if (!g.is_cuda()) raise_type(name, (int)i, "must live in device memory");
+            if (!is_kind(g.scalar_type(), kGrad)) raise_type(name, (int)i, "has dtype %s", at::toString(g.scalar_type()));
+            if (g.layout() != at::kStrided || !g.is_non_overlapping_and_dense()) raise_type(name, (int)i, "must be dense");
+            t.push_back(&g);
+            p.push_back(g.data_ptr());
+            dtype.push_back(grad_dtype(g.scalar_type()));
+            len.push_back((size_t)g.numel());
+        }
+    }
+};
+
+// (g, norm, workspace, stream)
+PyObject *grad_norm(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<4>(n, [&] {
+        float *norm = (float *)dev(a[1], kF32, 1, "norm");
+        void *ws = dev(a[2], kI64, ss_grad_norm_workspace_bytes() / 8, "workspace");
+        const hipStream_t s = stream_arg(a[3]);
+        const Gradients g(a[0], "g");
+        return unlocked([&] { return ss_grad_norm(g.p.data(), g.dtype.data(), g.len.data(), g.p.size(), norm, ws, s); });
+    });
+}
+
+// (g, norm, max_norm, out, stream); out None: in place
+PyObject *grad_clip(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<5>(n, [&] {
+        float *norm = (float *)dev(a[1], kF32, 1, "norm");
+        const float max_norm = float_arg(a[2]);
+        const hipStream_t s = stream_arg(a[4]);
+        const Gradients g(a[0], "g");
+        if (a[3] == Py_None)
+            return unlocked([&] {
+                return ss_grad_clip(g.p.data(), g.dtype.data(), g.len.data(), g.p.size(), norm, max_norm, g.p.data(), g.dtype.data(), s);
+            });
+        const Gradients out(a[3], "out");
+        if (out.p.size() != g.p.size()) {
+            PyErr_SetString(PyExc_ValueError, "g and out must have as many tensors");
+            throw PyRaised();
+        }
+        for (size_t i = 0; i < g.p.size(); ++i) {
+            if (out.len[i] != g.len[i]) raise_type("out", (int)i, "must have %zu elements", g.len[i]);
+            // element after element in memory: the same order on both sides
+            if (!(g.t[i]->is_contiguous() && out.t[i]->is_contiguous()) &&
+                !(g.t[i]->sizes() == out.t[i]->sizes() && g.t[i]->strides() == out.t[i]->strides()))
+                raise_type("out", (int)i, "must have g's memory order");
+        }
+        return unlocked([&] {
+            return ss_grad_clip(g.p.data(), g.dtype.data(), g.len.data(), g.p.size(), norm, max_norm, out.p.data(), out.dtype.data(), s);
+        });
+    });
+}
+
+// ---- matrices in MX4 ----
+
+// (data, scales, rows, cols), as binding.py's Mx4
+struct Mx4 {
+    uint8_t *data = nullptr, *scales = nullptr;
+    size_t rows = 0, cols = 0;
+    int device = -1;
+
+    Mx4() = default;
+    Mx4(PyObject *o, const char *name) {
+        if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) raise_type(name, -1, "must be an Mx4, got %s", Py_TYPE(o)->tp_name);
+        rows = size_arg(PyTuple_GET_ITEM(o, 2));
+        cols = size_arg(PyTuple_GET_ITEM(o, 3));
+        if (rows > SS_MX4_MAX_DIM || cols > SS_MX4_MAX_DIM) raise_type(name, -1, "has more rows or columns than %zu", SS_MX4_MAX_DIM);
+        data = bytes(PyTuple_GET_ITEM(o, 0), ss_mx4_data_bytes(rows, cols), name, "data");
+        scales = bytes(PyTuple_GET_ITEM(o, 1), ss_mx4_scale_bytes(rows, cols), name, "scales");
+        device = THPVariable_Unpack(PyTuple_GET_ITEM(o, 0)).device().index();
+    }
+    static uint8_t *bytes(PyObject *o, size_t n, const char *name, const char *field) {
+        char who[48];
+        snprintf(who, sizeof who, "%s.%s", name, field);
+        const at::Tensor &t = tensor(o, who);
+        if (!t.is_cuda()) raise_type(who, -1, "must live in device memory");
+        if (t.scalar_type() != at::kByte) raise_type(who, -1, "has dtype %s", at::toString(t.scalar_type()));
+        if (!t.is_contiguous() || (size_t)t.numel() < n) raise_type(who, -1, "must be contiguous with at least %zu bytes", n);
+        return (uint8_t *)t.data_ptr();
+    }
+    void shape(size_t r, size_t c, const char *name) const {
+        if (rows != r || cols != c) raise_type(name, -1, "must be %zu x %zu, got %zu x %zu", r, c, rows, cols);
+    }
+};
+
+// a plain matrix, its rows `ld` elements apart
+struct Matrix {
+    void *p;
+    ss_dtype dtype;
+    size_t rows, cols, ld;
+
+    Matrix(PyObject *o, const char *name) {
+        const at::Tensor &t = tensor(o, name);
+        if (!t.is_cuda()) raise_type(name, -1, "must live in device memory");
+        if (!is_kind(t.scalar_type(), kGrad)) raise_type(name, -1, "has dtype %s", at::toString(t.scalar_type()));
+        if (t.layout() != at::kStrided || t.dim() != 2) raise_type(name, -1, "must have two dimensions");
+        rows = (size_t)t.size(0);
+        cols = (size_t)t.size(1);
+        const int64_t apart = rows > 1 ? t.stride(0) : (int64_t)cols;
+        if ((cols > 1 && t.stride(1) != 1) || apart < (int64_t)cols) raise_type(name, -1, "must have the elements of a row side by side");
+        ld = (size_t)apart;
+        p = t.data_ptr();
+        dtype = grad_dtype(t.scalar_type());
+    }
+    void shape(size_t r, size_t c, const char *name) const {
+        if (rows != r || cols != c) raise_type(name, -1, "must be %zu x %zu, got %zu x %zu", r, c, rows, cols);
+    }
+};
+
+// (x, q, qt, stream)
+PyObject *mx4_quantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<4>(n, [&] {
+        const Matrix x(a[0], "x");
+        const Mx4 q = a[1] == Py_None ? Mx4() : Mx4(a[1], "q"), qt = a[2] == Py_None ? Mx4() : Mx4(a[2], "qt");
+        if (a[1] != Py_None) q.shape(x.rows, x.cols, "q");
+        if (a[2] != Py_None) qt.shape(x.cols, x.rows, "qt");
+        const hipStream_t s = stream_arg(a[3]);
+        return unlocked([&] { return ss_mx4_quantize(x.p, x.dtype, x.rows, x.cols, x.ld, q.data, q.scales, qt.data, qt.scales, s); });
+    });
+}
+
+// (q, out, stream)
+PyObject *mx4_dequantize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<3>(n, [&] {
+        const Mx4 q(a[0], "q");
+        const Matrix out(a[1], "out");
+        out.shape(q.rows, q.cols, "out");
+        const hipStream_t s = stream_arg(a[2]);
+        return unlocked([&] { return ss_mx4_dequantize(q.data, q.scales, q.rows, q.cols, out.p, out.dtype, out.ld, s); });
+    });
+}
+
+// (a, b, out, stream)
+PyObject *mx4_matmul(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<4>(n, [&] {
+        const Mx4 x(a[0], "a"), y(a[1], "b");
+        if (x.cols != y.cols) raise_type("b", -1, "must have a's %zu columns, got %zu", x.cols, y.cols);
+        const Matrix out(a[2], "out");
+        out.shape(x.rows, y.rows, "out");
+        const hipStream_t s = stream_arg(a[3]);
+        const bool own = own_stream(a[3], s);
+        return unlocked([&] {
+            const Lent scratch(ss_mx4_matmul_scratch_bytes(x.rows, y.rows, x.cols), x.device, s, own);
+            return ss_mx4_matmul(x.data, x.scales, y.data, y.scales, x.rows, y.rows, x.cols, out.p, out.dtype, out.ld, scratch.p,
+                                 scratch.bytes, s);
+        });
+    });
+}
+
+// (x, w, out, stream)
+PyObject *mx4_linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<4>(n, [&] {
+        const Matrix x(a[0], "x");
+        const Mx4 w(a[1], "w");
+        const Matrix out(a[2], "out");
+        if (x.cols != w.cols) raise_type("w", -1, "must have x's %zu columns, got %zu", x.cols, w.cols);
+        out.shape(x.rows, w.rows, "out");
+        const hipStream_t s = stream_arg(a[3]);
+        return unlocked([&] {
+            return ss_mx4_linear(x.p, x.dtype, x.rows, x.ld, w.data, w.scales, w.rows, w.cols, out.p, out.dtype, out.ld, s);
+        });
+    });
+}
+
 #define SS_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     SS_METHOD(signum_pack), SS_METHOD(majority_vote), SS_METHOD(vote_sum), SS_METHOD(sign_apply), SS_METHOD(sum_apply),
     SS_METHOD(signum_vote_step), SS_METHOD(stream_copy), SS_METHOD(welford_update), SS_METHOD(welford_sigma),
     SS_METHOD(density), SS_METHOD(signum_pack_ternary), SS_METHOD(quorum_vote), SS_METHOD(ternary_apply),
-    SS_METHOD(signum_vote_step_ternary), {nullptr, nullptr, 0, nullptr}};
+    SS_METHOD(signum_vote_step_ternary), SS_METHOD(grad_norm), SS_METHOD(grad_clip), SS_METHOD(mx4_quantize),
+    SS_METHOD(mx4_dequantize), SS_METHOD(mx4_matmul), SS_METHOD(mx4_linear), {nullptr, nullptr, 0, nullptr}};
 #undef SS_METHOD
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", "torch tensors to the C ABI of libsignsgd.so", -1, kMethods,

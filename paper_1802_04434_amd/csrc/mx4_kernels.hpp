@@ -1,0 +1,459 @@
+// Matrices in microscaled 4-bit floating point (E2M1 codes, one power of two for 32 of them): quantisation along rows and
+// down columns, the values back, the product A B^T, and the product with a few rows that are quantised on the way.
+//
+// The matrix unit takes the codes and the scales as they are stored: v_mfma_scale_f32_32x32x64_f8f6f4 multiplies 32 x 64 by
+// 64 x 32 codes, each lane giving the 32 codes (16 bytes) of one row's block and that block's scale byte, which the
+// instruction picks out of a register of four.  Which 32 of the columns a lane's block is makes no difference as long as
+// both operands take the same; so a lane takes four blocks that lie side by side, 64 bytes of codes and one
+// dword of scales, and the scales are stored as those dwords, a wave's rows after one another.
+#pragma once
+#include "common.hpp"
+
+#pragma clang fp contract(off)
+
+namespace mx4 {
+
+using ss::f32x4;
+using ss::u32x4;
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+// plain matrices are aligned to their element alone
+typedef u32x4 u32x4_f32 __attribute__((aligned(4)));
+typedef u32x4 u32x4_bf16 __attribute__((aligned(2)));
+
+constexpr uint32_t kBlockCols = 32;     // codes that share a scale
+constexpr uint32_t kGroupCols = 128;    // columns whose scales are one dword
+constexpr uint32_t kGroupBytes = 64;    // and their codes
+
+// ------------------------------------------------------------ quantise ----
+
+// The scale's byte for a block whose largest magnitude has these bits: floor(log2) - 2, at least 0 (2^-127); 127 for a block of
+// zeros; 255 where there is an infinity or a NaN.  The exponent of a subnormal reads as 0, and so does its byte.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t bits) {
+    const uint32_t e = bits >> 23;
+    const uint32_t byte = e > 2u ? e - 2u : 0u;
+    return bits == 0u ? 127u : e == 255u ? 255u : byte;
+}
+
+// 2^(byte - 127); infinity for 255
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+
+__device__ __forceinline__ uint32_t dpp_xor1(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1 /* quad_perm [1,0,3,2] */, 0xF, 0xF, false); }
+__device__ __forceinline__ uint32_t dpp_xor2(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E /* quad_perm [2,3,0,1] */, 0xF, 0xF, false); }
+__device__ __forceinline__ uint32_t dpp_mirror8(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141 /* row_half_mirror */, 0xF, 0xF, false); }
+__device__ __forceinline__ uint32_t dpp_mirror16(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140 /* row_mirror */, 0xF, 0xF, false); }
+
+__device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
+__device__ __forceinline__ uint32_t pk_umax16(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
+// 16 bytes of a row: four fp32 or eight bf16.  Magnitudes are compared as integers, in which infinities and NaN are largest.
+struct F32 {
+    typedef float elem;
+    static constexpr uint32_t kPer = 4, kLanes = 8;            // elements a lane, lanes a block
+    static __device__ __forceinline__ u32x4 load(const void *p) { return *static_cast<const u32x4_f32 *>(p); }
+    static __device__ __forceinline__ u32x4 magnitudes(u32x4 v) { return v & 0x7FFFFFFFu; }
+    static __device__ __forceinline__ u32x4 larger(u32x4 a, u32x4 b) { return __builtin_elementwise_max(a, b); }
+    // bits of the largest of 32, as an fp32, in all of their lanes
+    static __device__ __forceinline__ uint32_t row_max(u32x4 m) {
+        uint32_t v = umax(umax(m[0], m[1]), umax(m[2], m[3]));
+        v = umax(v, dpp_xor1(v));
+        v = umax(v, dpp_xor2(v));
+        return umax(v, dpp_mirror8(v));
+    }
+    // bits of element c's magnitude, as an fp32
+    static __device__ __forceinline__ uint32_t pick(u32x4 m, int c) { return m[c]; }
+    static __device__ __forceinline__ uint32_t row_codes(u32x4 v, float scale) {
+        uint32_t o = 0;
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[0]), __uint_as_float(v[1]), scale, 0);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[2]), __uint_as_float(v[3]), scale, 1);
+    }
+    static __device__ __forceinline__ void store_row_codes(uint8_t *p, uint32_t codes) { *reinterpret_cast<uint16_t *>(p) = (uint16_t)codes; }
+    // codes of element c in eight rows
+    static __device__ __forceinline__ uint32_t column_codes(const u32x4 *v, int c, float scale) {
+        uint32_t o = 0;
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[0][c]), __uint_as_float(v[1][c]), scale, 0);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[2][c]), __uint_as_float(v[3][c]), scale, 1);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[4][c]), __uint_as_float(v[5][c]), scale, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[6][c]), __uint_as_float(v[7][c]), scale, 3);
+    }
+    // the four scale bytes of 128 columns as a dword, in all of their 32 lanes
+    static __device__ __forceinline__ uint32_t gather_bytes(uint32_t byte, uint32_t lane) {
+        uint32_t v = byte << ((lane >> 3 & 3u) * 8);
+        v |= dpp_mirror16(v);
+        return v | (uint32_t)__shfl_xor((int)v, 16);
+    }
+};
+
+struct Bf16 {
+    typedef uint16_t elem;
+    static constexpr uint32_t kPer = 8, kLanes = 4;
+    static __device__ __forceinline__ u32x4 load(const void *p) { return *static_cast<const u32x4_bf16 *>(p); }
+    static __device__ __forceinline__ u32x4 magnitudes(u32x4 v) { return v & 0x7FFF7FFFu; }
+    static __device__ __forceinline__ u32x4 larger(u32x4 a, u32x4 b) {
+        u32x4 o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = pk_umax16(a[k], b[k]);
+        return o;
+    }
+    static __device__ __forceinline__ uint32_t row_max(u32x4 m) {
+        uint32_t v = pk_umax16(pk_umax16(m[0], m[1]), pk_umax16(m[2], m[3]));
+        v = pk_umax16(v, dpp_xor1(v));
+        v = pk_umax16(v, dpp_xor2(v));
+        return umax(v << 16, v & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ uint32_t pick(u32x4 m, int c) { return c & 1 ? m[c >> 1] & 0xFFFF0000u : m[c >> 1] << 16; }
+    static __device__ __forceinline__ bf16x2 pair(uint32_t v) { return __builtin_bit_cast(bf16x2, v); }
+    static __device__ __forceinline__ uint32_t row_codes(u32x4 v, float scale) {
+        uint32_t o = 0;
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, pair(v[0]), scale, 0);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, pair(v[1]), scale, 1);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, pair(v[2]), scale, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, pair(v[3]), scale, 3);
+    }
+    static __device__ __forceinline__ void store_row_codes(uint8_t *p, uint32_t codes) { *reinterpret_cast<uint32_t *>(p) = codes; }
+    static __device__ __forceinline__ uint32_t column_codes(const u32x4 *v, int c, float scale) {
+        uint32_t o = 0;
+        // the two rows' halves side by side
+        auto two = [&](int r) {
+            return pair(__builtin_amdgcn_perm(v[r + 1][c >> 1], v[r][c >> 1], c & 1 ? 0x07060302u : 0x05040100u));
+        };
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, two(0), scale, 0);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, two(2), scale, 1);
+        o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, two(4), scale, 2);
+        return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, two(6), scale, 3);
+    }
+    static __device__ __forceinline__ uint32_t gather_bytes(uint32_t byte, uint32_t lane) {
+        uint32_t v = byte << ((lane >> 2 & 3u) * 8);
+        v |= dpp_mirror8(v);
+        return v | dpp_mirror16(v);
+    }
+};
+
+struct QuantizeArgs {
+    const void *x;
+    uint8_t *data;             // NULL: not wanted
+    uint32_t *scales;
+    uint8_t *data_t;
+    uint32_t *scales_t;
+    size_t ld;
+    uint32_t rows, cols;
+    uint32_t chunks;           // of 64 lanes' columns
+};
+
+// kPer elements of row `row` from column `col` on, zeros where the matrix ends
+template <typename T>
+__device__ __forceinline__ u32x4 load_part(const QuantizeArgs &a, uint32_t row, uint32_t col) {
+    u32x4 v = {0, 0, 0, 0};
+    if (row >= a.rows) return v;
+    const typename T::elem *p = static_cast<const typename T::elem *>(a.x) + (size_t)row * a.ld + col;
+    if (col + T::kPer <= a.cols) return T::load(p);
+#pragma unroll
+    for (uint32_t k = 0; k < T::kPer; ++k)
+        if (col + k < a.cols) {
+            const uint32_t e = sizeof(p[0]) == 2 ? (uint32_t)reinterpret_cast<const uint16_t *>(p)[k] : reinterpret_cast<const uint32_t *>(p)[k];
+            if constexpr (sizeof(p[0]) == 2) v[k >> 1] |= e << (16 * (k & 1));
+            else v[k] = e;
+        }
+    return v;
+}
+
+// Along the rows alone: a wave takes R rows of 64 lanes' columns, four waves a block one below the other.
+template <typename T, int R>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t chunk = blockIdx.x % a.chunks, row0 = (blockIdx.x / a.chunks * 4 + wave) * R;
+    const uint32_t col = (chunk * 64 + lane) * T::kPer, padded = (a.cols + 127u) & ~127u;
+    u32x4 v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = load_part<T>(a, row0 + r, col);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t byte = scale_byte(T::row_max(T::magnitudes(v[r])));
+        const uint32_t codes = T::row_codes(v[r], scale_of(byte)), four = T::gather_bytes(byte, lane);
+        const uint32_t row = row0 + r;
+        if (row < a.rows && col < padded) {
+            T::store_row_codes(a.data + (size_t)row * (padded / 2) + col / 2, codes);
+            if ((lane & (4 * T::kLanes - 1)) == 0) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = four;
+        }
+    }
+}
+
+// Down the columns, and along the rows too where wanted, in one pass: a wave holds 32 rows of 64 lanes' columns in registers, so that a
+// column's block is one lane's and a row's is kLanes'.  Four waves of a block take 128 rows, whose scales are one dword a column.
+template <typename T, bool ROWS>
+__global__ __launch_bounds__(256) void quantize_both_kernel(const QuantizeArgs a) {
+    constexpr int R = 32;
+    __shared__ uint8_t bytes_t[64 * T::kPer * 4];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t chunk = blockIdx.x % a.chunks, band = blockIdx.x / a.chunks, row0 = band * 128 + wave * R;
+    const uint32_t col = (chunk * 64 + lane) * T::kPer, padded = (a.cols + 127u) & ~127u;
+    u32x4 v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) v[r] = load_part<T>(a, row0 + r, col);
+    if constexpr (ROWS) {
+        constexpr uint32_t kGroupLanes = 4 * T::kLanes;        // whose blocks share a dword: 32 or 16
+        uint32_t kept[R / kGroupLanes] = {};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const uint32_t byte = scale_byte(T::row_max(T::magnitudes(v[r])));
+            const uint32_t codes = T::row_codes(v[r], scale_of(byte)), four = T::gather_bytes(byte, lane);
+            const uint32_t row = row0 + r;
+            if (row < a.rows && col < padded) T::store_row_codes(a.data + (size_t)row * (padded / 2) + col / 2, codes);
+            // lane r of the group keeps row r's, so that they leave side by side
+            if ((lane & (kGroupLanes - 1)) == r % kGroupLanes) kept[r / kGroupLanes] = four;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < R / kGroupLanes; ++k) {
+            const uint32_t row = row0 + k * kGroupLanes + (lane & (kGroupLanes - 1));
+            if (row < a.rows && col < padded) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = kept[k];
+        }
+    }
+    u32x4 m = T::magnitudes(v[0]);
+#pragma unroll
+    for (int r = 1; r < R; ++r) m = T::larger(m, T::magnitudes(v[r]));
+    const size_t padded_rows = ((size_t)a.rows + 127) & ~(size_t)127;
+#pragma unroll
+    for (int c = 0; c < (int)T::kPer; ++c) {
+        const uint32_t byte = scale_byte(T::pick(m, c));
+        const float scale = scale_of(byte);
+        u32x4 codes;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) codes[k] = T::column_codes(v + 8 * k, c, scale);
+        if (col + c < a.cols) *reinterpret_cast<u32x4 *>(a.data_t + (size_t)(col + c) * (padded_rows / 2) + row0 / 2) = codes;
+        bytes_t[(lane * T::kPer + c) * 4 + wave] = (uint8_t)byte;
+    }
+    __syncthreads();
+    const uint32_t *fours = reinterpret_cast<const uint32_t *>(bytes_t);
+    for (uint32_t c = threadIdx.x; c < 64 * T::kPer; c += 256) {
+        const uint32_t to = chunk * 64 * T::kPer + c;
+        if (to < a.cols) a.scales_t[(size_t)band * a.cols + to] = fours[c];
+    }
+}
+
+// ---------------------------------------------------------- dequantise ----
+
+struct DequantizeArgs {
+    const uint8_t *data;
+    const uint8_t *scales;
+    void *out;
+    size_t ld;
+    uint32_t rows, cols;
+    uint32_t chunks;           // of 512 columns
+};
+
+// A lane takes eight codes, a wave R rows of 512 columns.
+template <bool OUT_BF16, int R>
+__global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs a) {
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
+    const uint32_t chunk = blockIdx.x % a.chunks, row0 = (blockIdx.x / a.chunks * 4 + wave) * R;
+    const uint32_t col = (chunk * 64 + lane) * 8, padded = (a.cols + 127u) & ~127u;
+    if (col >= a.cols) return;
+    uint32_t codes[R], bytes[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t row = row0 + r;
+        codes[r] = bytes[r] = 0;
+        if (row < a.rows) {
+            codes[r] = *reinterpret_cast<const uint32_t *>(a.data + (size_t)row * (padded / 2) + col / 2);
+            bytes[r] = a.scales[((size_t)(col / kGroupCols) * a.rows + row) * 4 + (col / kBlockCols & 3u)];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t row = row0 + r;
+        if (row >= a.rows) continue;
+        const float scale = scale_of(bytes[r]);
+        const bool nan = bytes[r] == 255u;
+        const size_t at = (size_t)row * a.ld + col;
+        if constexpr (OUT_BF16) {
+            u32x4 o;
+            o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[r], scale, 0));
+            o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[r], scale, 1));
+            o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[r], scale, 2));
+            o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[r], scale, 3));
+            if (nan) o = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
+            uint16_t *to = static_cast<uint16_t *>(a.out) + at;
+            if (col + 8 <= a.cols) *reinterpret_cast<u32x4_bf16 *>(to) = o;
+            else
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (col + k < a.cols) to[k] = (uint16_t)(o[k >> 1] >> (16 * (k & 1)));
+        } else {
+            f32x2 p[4];
+            p[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[r], scale, 0);
+            p[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[r], scale, 1);
+            p[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[r], scale, 2);
+            p[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[r], scale, 3);
+            u32x4 o[2];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k >> 2][k & 3] = nan ? 0x7FC00000u : __float_as_uint(p[k >> 1][k & 1]);
+            uint32_t *to = static_cast<uint32_t *>(a.out) + at;
+            if (col + 8 <= a.cols) {
+                reinterpret_cast<u32x4_f32 *>(to)[0] = o[0];
+                reinterpret_cast<u32x4_f32 *>(to)[1] = o[1];
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (col + k < a.cols) to[k] = o[k >> 2][k & 3];
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------- product ----
+
+__device__ __forceinline__ i32x8 widened(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
+
+// four steps of 64: block k of each lane's four, scaled by byte k of its dword (format 4: E2M1)
+__device__ __forceinline__ f32x16 multiply_32(const u32x4 *a, uint32_t sa, const u32x4 *b, uint32_t sb, f32x16 c) {
+    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[0]), widened(b[0]), c, 4, 4, 0, (int)sa, 0, (int)sb);
+    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[1]), widened(b[1]), c, 4, 4, 1, (int)sa, 1, (int)sb);
+    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[2]), widened(b[2]), c, 4, 4, 2, (int)sa, 2, (int)sb);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[3]), widened(b[3]), c, 4, 4, 3, (int)sa, 3, (int)sb);
+}
+__device__ __forceinline__ f32x4 multiply_16(const u32x4 *a, uint32_t sa, const u32x4 *b, uint32_t sb, f32x4 c) {
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[0]), widened(b[0]), c, 4, 4, 0, (int)sa, 0, (int)sb);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[1]), widened(b[1]), c, 4, 4, 1, (int)sa, 1, (int)sb);
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[2]), widened(b[2]), c, 4, 4, 2, (int)sa, 2, (int)sb);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[3]), widened(b[3]), c, 4, 4, 3, (int)sa, 3, (int)sb);
+}
+
+struct MatmulArgs {
+    const uint8_t *a, *b;
+    const uint32_t *sa, *sb;
+    void *out;
+    size_t ld;
+    uint32_t M, N;
+    uint32_t groups;           // of 128 columns
+    uint32_t tiles_n;
+};
+
+// the 64 bytes and the scales of one row and group; zeros beyond the matrix
+struct Part {
+    u32x4 v[4];
+    uint32_t s;
+    __device__ __forceinline__ void load(const uint8_t *data, const uint32_t *scales, uint32_t row, uint32_t rows, uint32_t group, uint32_t groups) {
+        s = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = u32x4{0, 0, 0, 0};
+        if (row >= rows || group >= groups) return;
+        const u32x4 *p = reinterpret_cast<const u32x4 *>(data + ((size_t)row * groups + group) * kGroupBytes);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = p[k];
+        s = scales[(size_t)group * rows + row];
+    }
+};
+
+template <bool OUT_BF16>
+__device__ __forceinline__ void store_out(void *out, size_t at, float v) {
+    if constexpr (OUT_BF16) static_cast<__bf16 *>(out)[at] = (__bf16)v;
+    else static_cast<float *>(out)[at] = v;
+}
+
+// one wave, 32 x 32 of the result
+template <bool OUT_BF16>
+__global__ __launch_bounds__(64) void matmul_kernel(const MatmulArgs a) {
+    const uint32_t lane = threadIdx.x, r = lane & 31u, q = lane >> 5;
+    const uint32_t m0 = blockIdx.x / a.tiles_n * 32, n0 = blockIdx.x % a.tiles_n * 32;
+    f32x16 c = {};
+    for (uint32_t g = 0; g < a.groups; g += 2) {
+        Part x, y;
+        x.load(a.a, a.sa, m0 + r, a.M, g + q, a.groups);
+        y.load(a.b, a.sb, n0 + r, a.N, g + q, a.groups);
+        c = multiply_32(x.v, x.s, y.v, y.s, c);
+    }
+    const uint32_t n = n0 + r;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t m = m0 + 8 * (i / 4) + 4 * q + i % 4;
+        if (m < a.M && n < a.N) store_out<OUT_BF16>(a.out, (size_t)m * a.ld + n, c[i]);
+    }
+}
+
+// ------------------------------------------------- product of a few rows ----
+
+struct LinearArgs {
+    const void *x;
+    const uint8_t *w;
+    const uint32_t *sw;
+    void *out;
+    size_t ldx, ldo;
+    uint32_t T, N, K, groups;
+    uint32_t first;            // row of w that the launch begins with
+};
+
+// One row's group of x in MX4, in one lane: its 128 columns as 32-column blocks, each quantised by itself.
+template <typename T>
+__device__ __forceinline__ void quantize_group(const LinearArgs &a, uint32_t row, uint32_t group, u32x4 *codes, uint32_t &scales) {
+    constexpr int kVecs = kBlockCols / T::kPer;
+    scales = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) codes[k] = u32x4{0, 0, 0, 0};
+    if (row >= a.T || group >= a.groups) return;
+    QuantizeArgs part{};
+    part.x = a.x;
+    part.ld = a.ldx;
+    part.rows = a.T;
+    part.cols = a.K;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        u32x4 v[kVecs];
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) v[i] = load_part<T>(part, row, group * kGroupCols + k * kBlockCols + i * T::kPer);
+        u32x4 m = T::magnitudes(v[0]);
+#pragma unroll
+        for (int i = 1; i < kVecs; ++i) m = T::larger(m, T::magnitudes(v[i]));
+        uint32_t bits = T::pick(m, 0);
+#pragma unroll
+        for (int c = 1; c < (int)T::kPer; ++c) bits = umax(bits, T::pick(m, c));
+        const uint32_t byte = scale_byte(bits);
+        const float scale = scale_of(byte);
+        scales |= byte << (8 * k);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+            const uint32_t c = T::row_codes(v[i], scale);
+            if constexpr (T::kPer == 8) codes[k][i] = c;
+            else codes[k][i / 2] |= c << (16 * (i & 1));
+        }
+    }
+}
+
+constexpr int kLinearWaves = 8;
+
+// A block takes 16 rows of w, its waves a share of the columns each; their sums are added through LDS in order.
+template <typename T, bool OUT_BF16>
+__global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearArgs a) {
+    __shared__ f32x4 part[kLinearWaves][64];
+    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, q = lane >> 4;
+    const uint32_t n0 = a.first + blockIdx.x * 16;
+    const uint32_t steps = (a.groups + 3) / 4, from = steps * wave / kLinearWaves, to = steps * (wave + 1) / kLinearWaves;
+    f32x4 c = {0, 0, 0, 0};
+    for (uint32_t s = from; s < to; ++s) {
+        Part w;
+        u32x4 x[4];
+        uint32_t sx;
+        w.load(a.w, a.sw, n0 + r, a.N, 4 * s + q, a.groups);
+        quantize_group<T>(a, r, 4 * s + q, x, sx);
+        c = multiply_16(x, sx, w.v, w.s, c);
+    }
+    part[wave][lane] = c;
+    __syncthreads();
+    if (wave) return;
+#pragma unroll
+    for (int k = 1; k < kLinearWaves; ++k) c += part[k][lane];
+    const uint32_t n = n0 + r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t t = 4 * q + i;
+        if (t < a.T && n < a.N) store_out<OUT_BF16>(a.out, (size_t)t * a.ldo + n, c[i]);
+    }
+}
+
+}  // namespace mx4

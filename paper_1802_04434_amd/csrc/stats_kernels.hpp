@@ -151,30 +151,6 @@ __device__ __forceinline__ void accumulate(float v, double &l1, double &l2sq) {
     l2sq = __builtin_fma(a, a, l2sq);
 }
 
-// another lane's value, zero in the rows (of 16 lanes) that ROWS leaves out
-template <int CTRL, int ROWS = 0xF>
-__device__ __forceinline__ double lane_move(double v) {
-    const uint64_t u = __builtin_bit_cast(uint64_t, v);
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), CTRL, ROWS, 0xF, false);
-    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
-}
-
-// sum over each eight lanes, in all of them
-__device__ __forceinline__ double sum8(double s) {
-    s += lane_move<0xB1 /* quad_perm [1,0,3,2] */>(s);
-    s += lane_move<0x4E /* quad_perm [2,3,0,1] */>(s);
-    return s + lane_move<0x141 /* row_half_mirror */>(s);
-}
-
-// sum over the wave, in lane 63
-__device__ __forceinline__ double sum_wave(double s) {
-    s = sum8(s);
-    s += lane_move<0x140 /* row_mirror */>(s);
-    s += lane_move<0x142 /* row_bcast:15 */, 0xA>(s);
-    return s + lane_move<0x143 /* row_bcast:31 */, 0xC>(s);
-}
-
 __device__ __forceinline__ void density_result(const DensityArgs &a, double s1, double s2) {
     a.out[0] = s1;
     a.out[1] = s2;
