@@ -421,13 +421,15 @@ int ss_mx4_dequantize(const uint8_t *data, const uint8_t *scales, size_t rows, s
 
 /*
  * out (M x N, a row every ld elements) <- a b^T, a of M x K and b of N x K in MX4.  Products are
- * exact, sums in fp32, rounded once to the type of out.  K = 0 gives zeros.
+ * exact, sums in fp32, rounded once to the type of out.  K = 0 gives zeros; K beyond
+ * SS_MX4_MAX_SUM is SS_ERR_ARG.
  *   scratch  work  ss_mx4_matmul_scratch_bytes(M, N, K) bytes of device memory, 16-byte aligned,
  *                  contents immaterial before and after; untouched by others until the
  *                  enqueued work has run.  NULL or smaller: one launch, which takes longer where that
  *                  size is not 0 (small outputs with a long K).
  * The order of the sums depends on M, N, K and on whether scratch is given.
  */
+#define SS_MX4_MAX_SUM ((size_t)1 << 24)
 size_t ss_mx4_matmul_scratch_bytes(size_t M, size_t N, size_t K);
 int ss_mx4_matmul(const uint8_t *a_data, const uint8_t *a_scales, const uint8_t *b_data,
                   const uint8_t *b_scales, size_t M, size_t N, size_t K, void *out,

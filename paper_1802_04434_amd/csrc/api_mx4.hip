@@ -1,4 +1,7 @@
 // C ABI of the matrices in microscaled 4-bit floating point (see include/signsgd.h): validation, kernel selection and launch.
+#include <algorithm>
+#include <cmath>
+
 #include "api_common.hpp"
 #include "mx4_kernels.hpp"
 
@@ -17,6 +20,83 @@ inline Span matrix(const void *p, size_t rows, size_t cols, size_t ld, ss_dtype 
 
 inline bool bad_matrix(size_t rows, size_t cols, size_t ld) {
     return rows > SS_MX4_MAX_DIM || cols > SS_MX4_MAX_DIM || ld < cols || ld > ((size_t)1 << 40) || rows * cols > SS_MX4_MAX_ELEMENTS;
+}
+
+// How a product, or a part of one, is cut: tiles of 64 times `tile` squared, and the sum over the columns into `splits` parts
+struct Plan {
+    int tile;
+    size_t splits;
+    double us;
+};
+
+inline size_t tiles_of(size_t n, int tile) { return (n + 64 * (size_t)tile - 1) / (64 * (size_t)tile); }
+
+// What a launch takes by its shape, from products of 64 x 4096 x 4096 to 8192 x 8192 x 16384: us a step of 256 columns with one block on a compute unit
+// (large tiles: few on the card) and with as many as fit, and us a block besides, of which the second part is for writing the result.  Two launches cost 3 us more,
+// and the partial sums their bytes, written, read and joined at 2.5 TB/s.
+inline Plan plan_of(size_t M, size_t N, size_t K, bool may_split) {
+    const size_t steps = (groups_of(K) + 1) / 2;
+    constexpr struct {
+        int tile;
+        double fit, alone, full, starts, ends;
+    } kShapes[] = {{4, 1, 1.15, 1.65, 3.0, 7.0}, {2, 2, 0.58, 1.06, 2.0, 3.5}, {1, 4, 0.40, 0.87, 1.5, 1.0}};
+    Plan best{1, 1, 1e300};
+    for (const auto &s : kShapes) {
+        const size_t tiles = tiles_of(M, s.tile) * tiles_of(N, s.tile);
+        // no more parts than fill the card once
+        for (size_t splits = 1; splits == 1 || (may_split && splits * 2 <= steps && tiles * splits <= (size_t)(256 * s.fit)); splits *= 2) {
+            const double blocks = (double)(tiles * splits), each = (double)((steps + splits - 1) / splits);
+            auto round = [&](double load) {       // blocks a compute unit
+                const double crowd = s.fit == 1 ? load : load > 1 ? (load - 1) / (s.fit - 1) : 0;
+                return each * (s.alone + (s.full - s.alone) * crowd) + s.starts + s.ends * load / s.fit;
+            };
+            const double rounds = std::floor(blocks / (256 * s.fit)), rest = blocks / 256 - rounds * s.fit;
+            double us = rounds * round(s.fit) + (rest > 0 ? round(rest) : 0);
+            if (splits > 1) us += 3.0 + (double)(splits * M * N) * 4 / 2.5e6;
+            if (us < best.us) best = Plan{s.tile, splits, us};
+        }
+    }
+    return best;
+}
+
+// A part of the result with a plan of its own
+struct Part {
+    size_t m, n, M, N;
+    Plan plan;
+};
+
+// A tile that hangs over the edge costs as much as a whole one: where the rows or columns beyond the last whole large tile are few, smaller ones take them.
+inline int parts_of(Part (&parts)[3], size_t M, size_t N, size_t K, bool may_split) {
+    parts[0] = Part{0, 0, M, N, plan_of(M, N, K, may_split)};
+    double least = parts[0].plan.us;
+    int count = 1;
+    for (const size_t edge : {(size_t)256, (size_t)128}) {
+        for (int which = 1; which < 4; ++which) {
+            const size_t over_m = M % edge, over_n = N % edge;
+            if ((which & 1 && (M < edge || over_m == 0 || over_m > edge / 2)) || (which & 2 && (N < edge || over_n == 0 || over_n > edge / 2))) continue;
+            const size_t m = which & 1 ? M - over_m : M, n = which & 2 ? N - over_n : N;
+            Part tried[3] = {{0, 0, m, n, plan_of(m, n, K, may_split)}};
+            int c = 1;
+            if (m < M) tried[c] = Part{m, 0, M - m, N, plan_of(M - m, N, K, may_split)}, ++c;
+            if (n < N) tried[c] = Part{0, n, m, N - n, plan_of(m, N - n, K, may_split)}, ++c;
+            double us = 1.5 * (c - 1);
+            for (int k = 0; k < c; ++k) us += tried[k].plan.us;
+            if (us < least) {
+                least = us;
+                count = c;
+                std::copy(tried, tried + c, parts);
+            }
+        }
+    }
+    return count;
+}
+
+// bytes of partial sums; the parts are computed one after the other
+inline size_t scratch_of(const Part *parts, int count) {
+    size_t bytes = 0;
+    for (int k = 0; k < count; ++k)
+        if (parts[k].plan.splits > 1) bytes = std::max(bytes, parts[k].plan.splits * parts[k].M * parts[k].N * sizeof(float));
+    return bytes;
 }
 
 }  // namespace
@@ -79,12 +159,16 @@ int ss_mx4_dequantize(const uint8_t *data, const uint8_t *scales, size_t rows, s
                           : launch(mx4::dequantize_kernel<false, kRows>, grid, 0, stream, a, 256);
 }
 
-size_t ss_mx4_matmul_scratch_bytes(size_t, size_t, size_t) { return 0; }
+size_t ss_mx4_matmul_scratch_bytes(size_t M, size_t N, size_t K) {
+    if (M == 0 || N == 0 || bad_matrix(M, N, N) || K > SS_MX4_MAX_SUM) return 0;
+    Part parts[3];
+    return scratch_of(parts, parts_of(parts, M, N, K, true));
+}
 
 int ss_mx4_matmul(const uint8_t *a_data, const uint8_t *a_scales, const uint8_t *b_data, const uint8_t *b_scales, size_t M, size_t N,
                   size_t K, void *out, ss_dtype odt, size_t ld, void *scratch, size_t scratch_bytes, void *hip_stream) {
     if (odt != SS_F32 && odt != SS_BF16) return SS_ERR_DTYPE;
-    if (bad_matrix(M, N, ld) || K > SS_MX4_MAX_DIM) return SS_ERR_ARG;
+    if (bad_matrix(M, N, ld) || K > SS_MX4_MAX_SUM) return SS_ERR_ARG;
     if (M == 0 || N == 0) return SS_OK;
     if (!out || (K && (!a_data || !a_scales || !b_data || !b_scales))) return SS_ERR_NULL;
     if (!aligned16(a_data) || !aligned16(a_scales) || !aligned16(b_data) || !aligned16(b_scales) || !aligned16(scratch) ||
@@ -94,12 +178,32 @@ int ss_mx4_matmul(const uint8_t *a_data, const uint8_t *a_scales, const uint8_t 
                      span(b_data, ss_mx4_data_bytes(N, K), false), span(b_scales, ss_mx4_scale_bytes(N, K), false),
                      matrix(out, M, N, ld, odt, true), span(scratch, scratch_bytes, true)};
     if (written_spans_overlap(spans, 6)) return SS_ERR_ARG;
-    mx4::MatmulArgs a{a_data, b_data, reinterpret_cast<const uint32_t *>(a_scales), reinterpret_cast<const uint32_t *>(b_scales), out, ld,
-                      (uint32_t)M, (uint32_t)N, (uint32_t)groups_of(K), (uint32_t)((N + 31) / 32)};
-    const size_t grid = (M + 31) / 32 * a.tiles_n;
-    if (grid > ((size_t)1 << 26) - 1) return SS_ERR_ARG;
+    Part parts[3];
+    int count = parts_of(parts, M, N, K, scratch != nullptr);
+    if (scratch && scratch_of(parts, count) > scratch_bytes) count = parts_of(parts, M, N, K, false);
+    const size_t groups = groups_of(K);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    return odt == SS_BF16 ? launch(mx4::matmul_kernel<true>, grid, 0, stream, a, 64) : launch(mx4::matmul_kernel<false>, grid, 0, stream, a, 64);
+    for (int k = 0; k < count; ++k) {
+        const Part &part = parts[k];
+        const int tile = part.plan.tile;
+        const bool join = part.plan.splits > 1, bf16 = odt == SS_BF16 && !join;
+        void *to = static_cast<char *>(out) + (part.m * ld + part.n) * grad_bytes(odt);
+        mx4::TilesArgs a{a_data + part.m * groups * mx4::kGroupBytes, b_data + part.n * groups * mx4::kGroupBytes,
+                         reinterpret_cast<const uint32_t *>(a_scales) + part.m, reinterpret_cast<const uint32_t *>(b_scales) + part.n,
+                         join ? scratch : to, join ? part.N : ld, (uint32_t)part.M, (uint32_t)part.N, (uint32_t)M, (uint32_t)N, (uint32_t)groups,
+                         (uint32_t)tiles_of(part.M, tile), (uint32_t)tiles_of(part.N, tile), (uint32_t)part.plan.splits};
+        const auto kernel = tile == 4 ? (bf16 ? mx4::matmul_tiles_kernel<true, 4> : mx4::matmul_tiles_kernel<false, 4>)
+                            : tile == 2 ? (bf16 ? mx4::matmul_tiles_kernel<true, 2> : mx4::matmul_tiles_kernel<false, 2>)
+                                        : (bf16 ? mx4::matmul_tiles_kernel<true, 1> : mx4::matmul_tiles_kernel<false, 1>);
+        int rc = launch(kernel, (size_t)a.tiles_m * a.tiles_n * a.splits, 0, stream, a, 256);
+        if (rc != SS_OK) return rc;
+        if (!join) continue;
+        const mx4::JoinArgs j{static_cast<const float *>(scratch), to, ld, a.M, a.N, a.splits};
+        const size_t blocks = (part.M * part.N + 1023) / 1024;
+        rc = odt == SS_BF16 ? launch(mx4::join_kernel<true>, blocks, 0, stream, j, 256) : launch(mx4::join_kernel<false>, blocks, 0, stream, j, 256);
+        if (rc != SS_OK) return rc;
+    }
+    return SS_OK;
 }
 
 int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8_t *w_data, const uint8_t *w_scales, size_t N, size_t K,

@@ -7,6 +7,8 @@
 // both operands take the same; so a lane takes four blocks that lie side by side, 64 bytes of codes and one
 // dword of scales, and the scales are stored as those dwords, a wave's rows after one another.
 #pragma once
+#include <type_traits>
+
 #include "common.hpp"
 
 #pragma clang fp contract(off)
@@ -311,13 +313,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs a)
 
 __device__ __forceinline__ i32x8 widened(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
 
-// four steps of 64: block k of each lane's four, scaled by byte k of its dword (format 4: E2M1)
-__device__ __forceinline__ f32x16 multiply_32(const u32x4 *a, uint32_t sa, const u32x4 *b, uint32_t sb, f32x16 c) {
-    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[0]), widened(b[0]), c, 4, 4, 0, (int)sa, 0, (int)sb);
-    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[1]), widened(b[1]), c, 4, 4, 1, (int)sa, 1, (int)sb);
-    c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[2]), widened(b[2]), c, 4, 4, 2, (int)sa, 2, (int)sb);
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(a[3]), widened(b[3]), c, 4, 4, 3, (int)sa, 3, (int)sb);
-}
+// four steps of 128: block k of each lane's four, scaled by byte k of its dword (format 4: E2M1)
 __device__ __forceinline__ f32x4 multiply_16(const u32x4 *a, uint32_t sa, const u32x4 *b, uint32_t sb, f32x4 c) {
     c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[0]), widened(b[0]), c, 4, 4, 0, (int)sa, 0, (int)sb);
     c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[1]), widened(b[1]), c, 4, 4, 1, (int)sa, 1, (int)sb);
@@ -325,15 +321,225 @@ __device__ __forceinline__ f32x4 multiply_16(const u32x4 *a, uint32_t sa, const 
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[3]), widened(b[3]), c, 4, 4, 3, (int)sa, 3, (int)sb);
 }
 
-struct MatmulArgs {
+template <bool OUT_BF16>
+__device__ __forceinline__ void store_out(void *out, size_t at, float v) {
+    if constexpr (OUT_BF16) static_cast<__bf16 *>(out)[at] = (__bf16)v;
+    else static_cast<float *>(out)[at] = v;
+}
+
+// Tiles of 2 x 2 waves, each 32 T rows by 32 T columns of the result.  A step is two groups of 128 columns, multiplied in four quarters of 64; the
+// fragments of the next quarter are read while one is multiplied.  Of each of the tile's rows of an operand a step takes 128 bytes of codes, loaded
+// straight into LDS, which has room for five operands' steps: both of the one that is read, both of the next one and the first of the one
+// after that.  So there is always something to load: the second operand of the next step right after the last one's place is free, when it has
+// the rest of the step to arrive, then the first one of the step after it, spread over the multiplications.
+struct TilesArgs {
     const uint8_t *a, *b;
     const uint32_t *sa, *sb;
+    void *out;                 // or the partial sums, split after split
+    size_t ld;
+    uint32_t M, N;             // of this launch, which may be a part of the product
+    uint32_t rows_a, rows_b;   // of the operands: from one group's scales to the next one's
+    uint32_t groups;           // of 128 columns
+    uint32_t tiles_m, tiles_n;
+    uint32_t splits;
+};
+
+// a value that all lanes have, for the scalar unit
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
+// all but the last N loads of this wave are there (neither a barrier nor a read waits for loads into LDS by itself), and so is what it read from LDS
+template <int N>
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
+
+template <int T>
+struct Fragments {
+    u32x4 a[T], b[T];
+};
+
+// part of 2 T of the multiplications of a quarter; BYTE: which one, and of the scales' bytes
+template <int BYTE, int T>
+__device__ __forceinline__ void multiply(f32x16 (&c)[T][T], const Fragments<T> &f, const uint32_t (&s)[2 * T], int part) {
+#pragma unroll
+    for (int x = part * T / 2; x < (part + 1) * T / 2; ++x)
+        c[x / T][x % T] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(f.a[x / T]), widened(f.b[x % T]), c[x / T][x % T], 4, 4, BYTE, (int)s[x / T],
+                                                                          BYTE, (int)s[T + x % T]);
+}
+
+template <bool OUT_BF16, int T>
+__global__ __launch_bounds__(256, 1) void matmul_tiles_kernel(const TilesArgs p) {
+    constexpr uint32_t B = 64 * T, kRow = 2 * kGroupBytes, kUnit = B * kRow, kRing = 5 * kUnit;
+    __shared__ __attribute__((aligned(128))) char lds[kRing];
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+    const uint32_t r = lane & 31u, q = lane >> 5;
+    // neighbouring blocks go to the eight dies in turn: each die takes a run of tiles, four tile rows high
+    const uint32_t total = gridDim.x, die = blockIdx.x & 7u, share = total >> 3, more = total & 7u;
+    uint32_t at = die * share + (die < more ? die : more) + (blockIdx.x >> 3);
+    const uint32_t tiles = p.tiles_m * p.tiles_n, split = uniform(at / tiles);
+    at -= split * tiles;
+    constexpr uint32_t kHigh = 4;
+    const uint32_t band = uniform(at / (kHigh * p.tiles_n)), in = at - band * kHigh * p.tiles_n;
+    const uint32_t left = p.tiles_m - band * kHigh, high = left < kHigh ? left : kHigh, column = uniform(in / high);
+    const uint32_t m0 = (band * kHigh + in - column * high) * B, n0 = column * B;
+    const uint32_t steps = (p.groups + 1) / 2, each = uniform(steps / p.splits), over = steps - each * p.splits;
+    const uint32_t from = split * each + (split < over ? split : over), to = from + each + (split < over ? 1u : 0u);
+    const uint32_t row_bytes = p.groups * kGroupBytes;
+
+    // Where a lane's 16 bytes of eight rows come from: chunk c of row r goes to place c ^ (r / 2 & 7) of its row in LDS, so that the rows
+    // that a read takes together lie in different banks.  Rows beyond the matrix are its last one; they are not stored.
+    constexpr int L = B / 32;       // loads a wave for one operand's step
+    uint32_t from_a[L], from_b[L];
+    const uint32_t chunk = ((lane & 7u) ^ ((wave & 1u) * 4 + (lane >> 4))) * 16, last_a = p.M - 1 - m0, last_b = p.N - 1 - n0;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const uint32_t row = (wave + 4 * i) * 8 + (lane >> 3);
+        from_a[i] = (row < last_a ? row : last_a) * row_bytes + chunk;
+        from_b[i] = (row < last_b ? row : last_b) * row_bytes + chunk;
+    }
+    const ss::Window wa = ss::window(p.a, (size_t)m0 * row_bytes, (last_a + 1 < B ? last_a + 1 : B) * row_bytes);
+    const ss::Window wb = ss::window(p.b, (size_t)n0 * row_bytes, (last_b + 1 < B ? last_b + 1 : B) * row_bytes);
+    typedef __attribute__((address_space(3))) void *Lds;
+    // the last steps load the last one again, which nothing reads: a branch would part the loop
+    auto column_of = [&](uint32_t step) { return (int)((step < to ? step : to - 1) * kRow); };
+    auto fetch_a = [&](int i, uint32_t place, int column) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(wa, (Lds)(lds + place + (wave + 4 * i) * 1024), 16, (int)from_a[i], column, 0, 0);
+    };
+    auto fetch_b = [&](int i, uint32_t place, int column) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(wb, (Lds)(lds + place + (wave + 4 * i) * 1024), 16, (int)from_b[i], column, 0, 0);
+    };
+    // scales: a dword a row and group, straight into registers
+    const uint32_t ma = (wave & 1u) * T * 32, nb = (wave >> 1) * T * 32;
+    uint32_t at_a[T], at_b[T], s[2 * T], next[2 * T];
+#pragma unroll
+    for (int i = 0; i < T; ++i) {
+        const uint32_t m = ma + i * 32 + r, n = nb + i * 32 + r;
+        at_a[i] = ((m < last_a ? m : last_a) + m0 + q * p.rows_a) * 4;
+        at_b[i] = ((n < last_b ? n : last_b) + n0 + q * p.rows_b) * 4;
+    }
+    auto fetch_scales = [&](uint32_t (&to_s)[2 * T], uint32_t step) {
+        // Of a last step with one group the other one's scales read as zero on both sides: whatever codes stand in their place (the next row's), their
+        // products are below 2^-240 and leave every sum as it is.
+        const bool two = p.groups - 2 * step >= 2;
+        const ss::Window va = ss::window(p.sa, (size_t)(2 * step) * p.rows_a * 4, uniform((two ? p.rows_a + p.M : p.M) * 4));
+        const ss::Window vb = ss::window(p.sb, (size_t)(2 * step) * p.rows_b * 4, uniform((two ? p.rows_b + p.N : p.N) * 4));
+#pragma unroll
+        for (int i = 0; i < T; ++i) to_s[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(va, (int)at_a[i], 0, 0);
+#pragma unroll
+        for (int i = 0; i < T; ++i) to_s[T + i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(vb, (int)at_b[i], 0, 0);
+    };
+    // fragment i of quarter j, in the order in which they are wanted: each lane's block is chunk 4 q + j of its row
+    uint32_t of_quarter[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) of_quarter[j] = r * kRow + (((4 * q + j) ^ (r >> 1 & 7u)) * 16);
+    auto read = [&](Fragments<T> &f, int i, int j, uint32_t a, uint32_t b) {
+        if (i < T) f.b[i] = *reinterpret_cast<const u32x4 *>(lds + b + nb * kRow + of_quarter[j] + i * 32 * kRow);
+        else f.a[i - T] = *reinterpret_cast<const u32x4 *>(lds + a + ma * kRow + of_quarter[j] + (i - T) * 32 * kRow);
+    };
+    f32x16 c[T][T] = {};
+    if (from < to) {
+        Fragments<T> f0, f1;
+        uint32_t a = 0, b = kUnit, a1 = 2 * kUnit, b1 = 3 * kUnit, free = 4 * kUnit;     // places of this step's operands, the next one's, and of what comes next
+#pragma unroll
+        for (int i = 0; i < L; ++i) fetch_a(i, a, column_of(from)), fetch_b(i, b, column_of(from));
+        fetch_scales(s, from);
+        arrived<0>();
+        __builtin_amdgcn_s_barrier();
+#pragma unroll
+        for (int i = 0; i < L; ++i) fetch_a(i, a1, column_of(from + 1)), fetch_b(i, b1, column_of(from + 1));
+#pragma unroll
+        for (int i = 0; i < 2 * T; ++i) read(f0, i, 0, a, b);
+        __builtin_amdgcn_sched_barrier(0);
+        for (uint32_t step = from; step < to; ++step) {
+            const int column = column_of(step + 2);
+            // Part by part, with a read and perhaps a load in each: in one go they would keep the matrix unit waiting while their queues are full
+            fetch_scales(next, step + 1 < to ? step + 1 : step);
+#pragma unroll
+            for (int part = 0; part < 2 * T; ++part) {
+                read(f1, part, 1, a, b);
+                multiply<0>(c, f0, s, part);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int part = 0; part < 2 * T; ++part) {
+                read(f0, part, 2, a, b);
+                if (part % 2 == 0) fetch_a(part / 2, free, column);
+                multiply<1>(c, f1, s, part);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int part = 0; part < 2 * T; ++part) {
+                read(f1, part, 3, a, b);
+                if (part % 2 == 0) fetch_a(T + part / 2, free, column);
+                multiply<2>(c, f0, s, part);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            // this step's places have been read by all, and the next one's operands are there
+            arrived<L>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int part = 0; part < 2 * T; ++part) {
+                read(f0, part, 0, a1, b1);
+                fetch_b(part, a, column);
+                multiply<3>(c, f1, s, part);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * T; ++i) s[i] = next[i];
+            const uint32_t was_a = a, was_b = b;
+            a = a1, b = b1, a1 = free, b1 = was_a, free = was_b;
+        }
+        arrived<0>();       // nothing is on its way into LDS that the next block may have
+    }
+    const size_t base = (size_t)split * p.M * p.N;      // of partial sums; split is 0 where there are none
+    typedef typename std::conditional<OUT_BF16, __bf16, float>::type Out;
+    Out *out = static_cast<Out *>(p.out) + base + (size_t)(m0 + ma) * p.ld + n0 + nb + r;
+    const bool whole = last_a + 1 >= B && last_b + 1 >= B;
+#pragma unroll
+    for (int i = 0; i < T; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const uint32_t row = i * 32 + 8 * (e / 4) + 4 * q + e % 4;
+            Out *to_row = out + row * p.ld;
+            if (whole) {
+#pragma unroll
+                for (int k = 0; k < T; ++k) to_row[k * 32] = (Out)c[i][k][e];
+            } else if (ma + row <= last_a) {
+#pragma unroll
+                for (int k = 0; k < T; ++k)
+                    if (nb + k * 32 + r <= last_b) to_row[k * 32] = (Out)c[i][k][e];
+            }
+        }
+}
+
+struct JoinArgs {
+    const float *parts;
     void *out;
     size_t ld;
-    uint32_t M, N;
-    uint32_t groups;           // of 128 columns
-    uint32_t tiles_n;
+    uint32_t M, N, splits;
 };
+
+// the partial sums, one after the other: four columns a lane where rows are aligned to it, rows of a block by its number
+template <bool OUT_BF16>
+__global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
+    const size_t size = (size_t)p.M * p.N, at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= size) return;
+    const uint32_t n = size - at < 4 ? (uint32_t)(size - at) : 4u;
+    f32x4 s = {0, 0, 0, 0};
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    if (n == 4) {
+        for (uint32_t k = 0; k < p.splits; ++k) s += *reinterpret_cast<const f32x4_any *>(p.parts + k * size + at);
+    } else {
+        for (uint32_t k = 0; k < p.splits; ++k)
+            for (uint32_t i = 0; i < n; ++i) s[i] += p.parts[k * size + at + i];
+    }
+    uint32_t row = (uint32_t)(at / p.N), col = (uint32_t)(at - (size_t)row * p.N);
+    for (uint32_t i = 0; i < n; ++i) {
+        store_out<OUT_BF16>(p.out, (size_t)row * p.ld + col, s[i]);
+        if (++col == p.N) col = 0, ++row;
+    }
+}
+
+// ------------------------------------------------- product of a few rows ----
 
 // the 64 bytes and the scales of one row and group; zeros beyond the matrix
 struct Part {
@@ -351,33 +557,6 @@ struct Part {
     }
 };
 
-template <bool OUT_BF16>
-__device__ __forceinline__ void store_out(void *out, size_t at, float v) {
-    if constexpr (OUT_BF16) static_cast<__bf16 *>(out)[at] = (__bf16)v;
-    else static_cast<float *>(out)[at] = v;
-}
-
-// one wave, 32 x 32 of the result
-template <bool OUT_BF16>
-__global__ __launch_bounds__(64) void matmul_kernel(const MatmulArgs a) {
-    const uint32_t lane = threadIdx.x, r = lane & 31u, q = lane >> 5;
-    const uint32_t m0 = blockIdx.x / a.tiles_n * 32, n0 = blockIdx.x % a.tiles_n * 32;
-    f32x16 c = {};
-    for (uint32_t g = 0; g < a.groups; g += 2) {
-        Part x, y;
-        x.load(a.a, a.sa, m0 + r, a.M, g + q, a.groups);
-        y.load(a.b, a.sb, n0 + r, a.N, g + q, a.groups);
-        c = multiply_32(x.v, x.s, y.v, y.s, c);
-    }
-    const uint32_t n = n0 + r;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const uint32_t m = m0 + 8 * (i / 4) + 4 * q + i % 4;
-        if (m < a.M && n < a.N) store_out<OUT_BF16>(a.out, (size_t)m * a.ld + n, c[i]);
-    }
-}
-
-// ------------------------------------------------- product of a few rows ----
 
 struct LinearArgs {
     const void *x;

@@ -142,7 +142,7 @@ def check_matrices_are_refused(c):
     assert c.matmul(5, 6, 100, a=good, b=good)[0] == OK                         # read only: a product with itself
     for name in ("a", "sa", "b", "sb"):
         assert c.matmul(5, 6, 100, out=good + 16, **{name: good}) == (ARG, [])
-    assert c.matmul(5, 6, 100, ld=5) == (ARG, []) and c.matmul(5, 6, (1 << 27) + 1, a=good) == (ARG, []) and c.matmul(1 << 18, 1 << 18, 100, out=good) == (ARG, [])
+    assert c.matmul(5, 6, 100, ld=5) == (ARG, []) and c.matmul(5, 6, (1 << 24) + 1, a=good) == (ARG, []) and c.matmul(1 << 18, 1 << 18, 100, out=good) == (ARG, [])
     assert c.matmul(0, 6, 100) == (OK, []) and c.matmul(5, 0, 100) == (OK, []) and len(c.matmul(5, 6, 0)[1]) == 1
     for name in ("x", "w", "sw", "out"):
         assert c.linear(5, 6, 100, **{name: 0}) == (NULL, [])
@@ -167,7 +167,7 @@ def check_large_matrices_are_launched(c):
                 assert rc == OK and len(got) == 1 and 0 < threads(got[0]) < 1 << 32, (rows, cols, dt, want, rc)
             rc, got = c.dequantize(rows, cols, dt)
             assert rc == OK and len(got) == 1 and 0 < threads(got[0]) < 1 << 32, (rows, cols, dt, rc)
-    for M, N, K in ((1 << 27, 128, 128), (1 << 27, 1, 64), (1, 1 << 27, 64), (1 << 17, 1 << 17, 512), (16, 16, 1 << 27), (128, 1 << 27, 64)):
+    for M, N, K in ((1 << 27, 128, 128), (1 << 27, 1, 64), (1, 1 << 27, 64), (1 << 17, 1 << 17, 512), (16, 16, 1 << 24), (128, 1 << 27, 64)):
         for lend in (True, False):
             rc, got = c.matmul(M, N, K, BF16, lend=lend)
             assert rc == OK and got and all(0 < threads(t) < 1 << 32 for t in got), (M, N, K, rc)
