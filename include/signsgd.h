@@ -354,9 +354,11 @@ int ss_density_static(const float *v, size_t d, double *out, void *hip_stream);
  *   norm       out  one fp32 in DEVICE memory, 16-byte aligned
  *   workspace  i/o  ss_grad_norm_workspace_bytes() bytes of DEVICE memory, under the same
  *                   terms as that of ss_density
- * One launch for every SS_GRAD_TENSORS_PER_LAUNCH tensors.
+ * One launch for every SS_GRAD_NORM_PER_LAUNCH tensors that are not empty; should one be
+ * refused (SS_ERR_HIP), those before it stay enqueued and write nothing but the workspace,
+ * which stays ready.
  */
-#define SS_GRAD_TENSORS_PER_LAUNCH 176
+#define SS_GRAD_NORM_PER_LAUNCH 256
 size_t ss_grad_norm_workspace_bytes(void);
 int ss_grad_norm(const void *const *g, const ss_dtype *gdt, const size_t *len, size_t n,
                  float *norm, void *workspace, void *hip_stream);
@@ -372,7 +374,10 @@ int ss_grad_norm(const void *const *g, const ss_dtype *gdt, const size_t *len, s
  *                  apart from that nothing that is written may share a byte with
  *                  anything else of the call.  Parts of one vector: the gradients as a step
  *                  reads them.
+ * One launch for every SS_GRAD_CLIP_PER_LAUNCH tensors that are not empty; the ones before a refused
+ * launch stay enqueued.  SS_ERR_RANGE: no host memory to compare the tensors' addresses.
  */
+#define SS_GRAD_CLIP_PER_LAUNCH 176
 int ss_grad_clip(const void *const *g, const ss_dtype *gdt, const size_t *len, size_t n,
                  const float *norm, float max_norm, void *const *out, const ss_dtype *odt,
                  void *hip_stream);

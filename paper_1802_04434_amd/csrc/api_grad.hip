@@ -9,7 +9,7 @@ namespace {
 
 using namespace host;
 
-static_assert(grads::kTensors == SS_GRAD_TENSORS_PER_LAUNCH, "the header says how many");
+static_assert(grads::kNormTensors == SS_GRAD_NORM_PER_LAUNCH && grads::kClipTensors == SS_GRAD_CLIP_PER_LAUNCH, "the header says how many");
 static_assert(sizeof(grads::ClipArgs) <= 4096 && sizeof(grads::NormArgs) <= 4096, "argument block");
 
 // elements of one tensor, and bytes of all: no card holds more, and units stay below 2^32
@@ -18,6 +18,11 @@ constexpr size_t kMaxBytes = (size_t)1 << 42;
 
 // units of one launch of the clip: 2^32 - 1 threads at most
 constexpr size_t kClipGrid = ((size_t)1 << 32) / grads::kClipThreads - 1;
+
+inline size_t clip_unit(ss_dtype in, ss_dtype out) {
+    if (out == SS_BF16) return in == SS_BF16 ? grads::kClipUnit<true, true> : grads::kClipUnit<false, true>;
+    return in == SS_BF16 ? grads::kClipUnit<true, false> : grads::kClipUnit<false, false>;
+}
 
 int check_list(const void *const *g, const ss_dtype *gdt, const size_t *len, size_t n) {
     if (n == 0) return SS_OK;
@@ -70,6 +75,13 @@ struct Written {
     }
 };
 
+// Up to here the norm leaves the gradients in the memory-side cache, for the clip that reads them next.  us, norm and both, not kept / kept: 25.6 M fp32
+// 20.6 and 57.9 / 21.4 and 53.4, 50 M bf16 in 150 tensors 23.9 and 64.6 / 24.1 and 59.7; 1.5 G bf16 438 / 488.
+constexpr size_t kNormKeeps = (size_t)1 << 28;
+// From here on 256 blocks with eight units in flight, below 512 with four: us, 256 / 512: 1.5 G bf16 438 / 448; 138 M mixed 67.2 / 64.1, 25.6 M fp32 in 161 tensors 23.2 / 22.5,
+// 5 M in 900 36.6 / 29.9, 272,474 in 65 6.5 / 6.2.
+constexpr size_t kNormLarge = (size_t)1 << 30;
+
 }  // namespace
 
 extern "C" {
@@ -88,14 +100,9 @@ int ss_grad_norm(const void *const *g, const ss_dtype *gdt, const size_t *len, s
         const Span s = span(g[t], len[t] * grad_bytes(gdt[t]), false);
         if (share(s, out) || share(s, ws)) return SS_ERR_ARG;
     }
-    grads::NormArgs a;
-    a.norm = norm;
-    a.scratch = static_cast<grads::NormScratch *>(workspace);
-    size_t t = 0;
-    do {
-        a.opens = t == 0;
+    const auto take = [&](grads::NormArgs &a, size_t t) {      // the tensors of a launch that begins with t; where the next one does
         uint32_t units = 0;
-        for (a.n = 0; t < n && a.n < (uint32_t)grads::kTensors; ++t) {
+        for (a.n = 0; t < n && a.n < (uint32_t)grads::kNormTensors; ++t) {
             if (len[t] == 0) continue;
             const uint64_t at = address(g[t], gdt[t]);
             const size_t bytes = (size_t)(at & 14u) + len[t] * grad_bytes(gdt[t]);
@@ -106,12 +113,27 @@ int ss_grad_norm(const void *const *g, const ss_dtype *gdt, const size_t *len, s
             ++a.n;
         }
         a.first[a.n] = units;
-        a.closes = t == n;
-        const size_t grid = std::min<size_t>(std::max<uint32_t>(units, 1), grads::kNormBlocks);
-        const int launched = launch(grads::norm_kernel, grid, 0, static_cast<hipStream_t>(hip_stream), a, grads::kNormThreads);
-        if (launched != SS_OK) return launched;
-    } while (t < n);
-    return SS_OK;
+        while (t < n && len[t] == 0) ++t;
+        return t;
+    };
+    size_t bytes = 0;
+    for (size_t t = 0; t < n; ++t) bytes += len[t] * grad_bytes(gdt[t]);
+    const bool once = bytes > kNormKeeps, large = bytes >= kNormLarge;
+    const uint32_t most = large ? grads::kNormBlocks / 2 : grads::kNormBlocks;
+    const auto kernel = large ? grads::norm_kernel<8, true> : once ? grads::norm_kernel<4, true> : grads::norm_kernel<4, false>;
+    const auto blocks = [&](const grads::NormArgs &a) { return std::min(std::max<uint32_t>(a.first[a.n], 1), most); };
+    grads::NormArgs a;
+    a.norm = norm;
+    a.scratch = static_cast<grads::NormScratch *>(workspace);
+    size_t next = take(a, 0);
+    // of several launches the first one opens as many slots as the largest can need
+    a.slots = next < n ? most : blocks(a);
+    for (a.opens = 1;; a.opens = 0) {
+        a.closes = next == n;
+        const int launched = launch(kernel, a.opens ? a.slots : blocks(a), 0, static_cast<hipStream_t>(hip_stream), a, grads::kNormThreads);
+        if (launched != SS_OK || a.closes) return launched;
+        next = take(a, next);
+    }
 }
 
 int ss_grad_clip(const void *const *g, const ss_dtype *gdt, const size_t *len, size_t n, const float *norm, float max_norm,
@@ -137,23 +159,22 @@ int ss_grad_clip(const void *const *g, const ss_dtype *gdt, const size_t *len, s
     size_t t = 0, from = 0;
     while (t < n) {
         size_t units = 0;
-        for (a.n = 0; t < n && a.n < (uint32_t)grads::kTensors && units < kClipGrid;) {
+        for (a.n = 0; t < n && a.n < (uint32_t)grads::kClipTensors && units < kClipGrid;) {
             const size_t size = grad_bytes(gdt[t]), osize = grad_bytes(odt[t]), left = len[t] - from;
             if (left == 0) {
                 ++t;
                 from = 0;
                 continue;
             }
+            const size_t unit = clip_unit(gdt[t], odt[t]);
             const uint64_t in = reinterpret_cast<uint64_t>(g[t]) + from * size, to = reinterpret_cast<uint64_t>(out[t]) + from * osize;
-            const size_t lead = (to & 15u) / osize;
-            const size_t most = (kClipGrid - units) * grads::kClipUnit - lead, take = std::min(left, most);
-            const size_t elements = lead + take;
+            const size_t lead = (to & 15u) / osize, elements = std::min(lead + left, (kClipGrid - units) * unit);
             a.at[a.n] = in | (gdt[t] == SS_BF16 ? 1u : 0u);
             a.out[a.n] = to | (odt[t] == SS_BF16 ? 1u : 0u);
             a.first[a.n] = (uint32_t)units;
-            a.rest[a.n] = (uint16_t)((elements - 1) % grads::kClipUnit);
-            units += (elements + grads::kClipUnit - 1) / grads::kClipUnit;
-            from += take;
+            a.rest[a.n] = (uint16_t)((elements - 1) % unit);
+            units += (elements + unit - 1) / unit;
+            from += elements - lead;
             ++a.n;
         }
         if (a.n == 0) break;

@@ -222,3 +222,14 @@ def test_offsets_beyond_32_bits():
     assert same(flat[-4:].cpu(), torch.cat([clipped(g[0][-1:], float(norm), 1.0, torch.bfloat16), clipped(g[1], float(norm), 1.0, torch.bfloat16)]))
     assert same(flat[(1 << 31) + 7:(1 << 31) + 8].cpu(), clipped(g[0][(1 << 31) + 7:(1 << 31) + 8], float(norm), 1.0, torch.bfloat16))
     assert int(torch.count_nonzero(flat)) == 5
+
+
+@pytest.mark.parametrize("nbytes", [(1 << 28) - 64, 1 << 28, (1 << 28) + 64, (1 << 30) - 64, 1 << 30, (1 << 30) + 64])
+def test_norm_around_the_sizes_where_its_launch_changes(nbytes):
+    ws, norm = ss.new_grad_norm_workspace(), torch.empty(1, device=DEV)
+    for dtype, parts in ((torch.bfloat16, 1), (torch.float32, 3), (torch.bfloat16, 300)):
+        n = nbytes // (2 if dtype == torch.bfloat16 else 4)
+        flat = torch.randn(n, device=DEV).to(dtype)
+        g = list(flat.split([n - 1001 * (parts - 1)] + [1001] * (parts - 1)))
+        want = math.sqrt(sum(float(t.double().square().sum()) for t in flat.split(1 << 26)))
+        assert abs(float(ss.grad_norm(g, norm, ws)) - want) <= NORM * want

@@ -101,12 +101,13 @@ def check_lists_are_refused(c):
 
 
 def check_how_lists_are_launched(c):
-    per = int(re.search(r"SS_GRAD_TENSORS_PER_LAUNCH (\d+)", open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "signsgd.h")).read()).group(1))
-    for n, launches in ((0, 1), (1, 1), (per, 1), (per + 1, 2), (5 * per, 5)):
-        rc, got = c.norm([100] * n)
-        assert rc == OK and len(got) == launches and all(threads(t) < 1 << 32 for t in got)
-        rc, got = c.clip([100] * n)
-        assert rc == OK and len(got) == (launches if n else 0) and all(threads(t) < 1 << 32 for t in got)
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "signsgd.h")).read()
+    for call, name in ((c.norm, "NORM"), (c.clip, "CLIP")):
+        per = int(re.search(r"SS_GRAD_%s_PER_LAUNCH (\d+)" % name, header).group(1))
+        for n, launches in ((0, 1 if call == c.norm else 0), (1, 1), (per, 1), (per + 1, 2), (5 * per, 5)):
+            for lengths in ([100] * n, [0, 100, 0] * n):
+                rc, got = call(lengths)
+                assert rc == OK and len(got) == launches and all(0 < threads(t) < 1 << 32 for t in got), (name, n)
     assert c.norm([0] * 1000)[0] == OK and c.clip([0] * 1000) == (OK, [])
     # a tensor of a quarter of the card's memory and more, and many of them
     for lengths, types in (([1 << 36], [F32]), ([(1 << 37) - 3], [BF16]), ([(1 << 34) + 1] * 9, [BF16] * 9)):
