@@ -32,6 +32,9 @@ constexpr uint32_t kBlockCols = 32;     // codes that share a scale
 constexpr uint32_t kGroupCols = 128;    // columns whose scales are one dword
 constexpr uint32_t kGroupBytes = 64;    // and their codes
 
+// a value that all lanes have, for the scalar unit
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+
 // ------------------------------------------------------------ quantise ----
 
 // The scale's byte for a block whose largest magnitude has these bits: floor(log2) - 2, at least 0 (2^-127); 127 for a block of
@@ -59,7 +62,17 @@ __device__ __forceinline__ uint32_t pk_umax16(uint32_t a, uint32_t b) {
 struct F32 {
     typedef float elem;
     static constexpr uint32_t kPer = 4, kLanes = 8;            // elements a lane, lanes a block
-    static __device__ __forceinline__ u32x4 load(const void *p) { return *static_cast<const u32x4_f32 *>(p); }
+    template <bool ONCE = false>
+    static __device__ __forceinline__ u32x4 load(const void *p) {
+        const u32x4_f32 *q = static_cast<const u32x4_f32 *>(p);
+        return ONCE ? __builtin_nontemporal_load(q) : *q;
+    }
+    // without the first s elements, zeros behind
+    static __device__ __forceinline__ u32x4 drop(u32x4 v, uint32_t s) {
+        if (s & 1u) v = u32x4{v[1], v[2], v[3], 0};
+        if (s & 2u) v = u32x4{v[2], v[3], 0, 0};
+        return v;
+    }
     static __device__ __forceinline__ u32x4 magnitudes(u32x4 v) { return v & 0x7FFFFFFFu; }
     static __device__ __forceinline__ u32x4 larger(u32x4 a, u32x4 b) { return __builtin_elementwise_max(a, b); }
     // bits of the largest of 32, as an fp32, in all of their lanes
@@ -96,7 +109,17 @@ struct F32 {
 struct Bf16 {
     typedef uint16_t elem;
     static constexpr uint32_t kPer = 8, kLanes = 4;
-    static __device__ __forceinline__ u32x4 load(const void *p) { return *static_cast<const u32x4_bf16 *>(p); }
+    template <bool ONCE = false>
+    static __device__ __forceinline__ u32x4 load(const void *p) {
+        const u32x4_bf16 *q = static_cast<const u32x4_bf16 *>(p);
+        return ONCE ? __builtin_nontemporal_load(q) : *q;
+    }
+    static __device__ __forceinline__ u32x4 drop(u32x4 v, uint32_t s) {
+        if (s & 1u) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+        if (s & 2u) v = u32x4{v[1], v[2], v[3], 0};
+        if (s & 4u) v = u32x4{v[2], v[3], 0, 0};
+        return v;
+    }
     static __device__ __forceinline__ u32x4 magnitudes(u32x4 v) { return v & 0x7FFF7FFFu; }
     static __device__ __forceinline__ u32x4 larger(u32x4 a, u32x4 b) {
         u32x4 o;
@@ -149,7 +172,7 @@ struct QuantizeArgs {
     uint32_t chunks;           // of 64 lanes' columns
 };
 
-// kPer elements of row `row` from column `col` on, zeros where the matrix ends
+// kPer elements of row `row` from column `col` on, one by one; zeros where the matrix ends
 template <typename T>
 __device__ __forceinline__ u32x4 load_part(const QuantizeArgs &a, uint32_t row, uint32_t col) {
     u32x4 v = {0, 0, 0, 0};
@@ -166,77 +189,136 @@ __device__ __forceinline__ u32x4 load_part(const QuantizeArgs &a, uint32_t row, 
     return v;
 }
 
-// Along the rows alone: a wave takes R rows of 64 lanes' columns, four waves a block one below the other.
-template <typename T, int R>
-__global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a) {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t chunk = blockIdx.x % a.chunks, row0 = (blockIdx.x / a.chunks * 4 + wave) * R;
-    const uint32_t col = (chunk * 64 + lane) * T::kPer, padded = (a.cols + 127u) & ~127u;
-    u32x4 v[R];
+// R rows' parts, out together; INSIDE: nothing ends in them.  The rows are the same for all lanes, so that their addresses are the scalar unit's.  Where the
+// matrix ends a lane loads what ends with it and drops the front, so that no load waits for a test: waited for one by one 16 rows took 8 us.
+template <typename T, int R, bool INSIDE, bool ONCE>
+__device__ __forceinline__ void load_rows(u32x4 (&v)[R], const QuantizeArgs &a, uint32_t row0, uint32_t col) {
+    const typename T::elem *x = static_cast<const typename T::elem *>(a.x);
+    if (!INSIDE && a.cols < T::kPer) {
 #pragma unroll
-    for (int r = 0; r < R; ++r) v[r] = load_part<T>(a, row0 + r, col);
+        for (int r = 0; r < R; ++r) v[r] = load_part<T>(a, row0 + r, col);
+        return;
+    }
+    const uint32_t from = INSIDE || col + T::kPer <= a.cols ? col : a.cols - T::kPer, over = col - from;      // kPer and more: nothing left
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const uint32_t row = INSIDE || row0 + r < a.rows ? row0 + r : a.rows - 1;
+        v[r] = T::template load<ONCE>(x + (size_t)row * a.ld + from);
+    }
+    if (INSIDE) return;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if (a.cols % T::kPer) v[r] = T::drop(v[r], over);
+        const bool none = row0 + r >= a.rows || over >= T::kPer;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[r][k] = none ? 0u : v[r][k];
+    }
+}
+
+// Along the rows alone: a wave takes R rows of 64 lanes' columns, four waves a block one below the other.
+template <typename T, int R, bool ONCE, bool INSIDE>
+__device__ __forceinline__ void quantize_rows(const QuantizeArgs &a, uint32_t lane, uint32_t row0, uint32_t col) {
+    const uint32_t padded = (a.cols + 127u) & ~127u;
+    u32x4 v[R];
+    load_rows<T, R, INSIDE, ONCE>(v, a, row0, col);
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const uint32_t byte = scale_byte(T::row_max(T::magnitudes(v[r])));
         const uint32_t codes = T::row_codes(v[r], scale_of(byte)), four = T::gather_bytes(byte, lane);
         const uint32_t row = row0 + r;
-        if (row < a.rows && col < padded) {
+        if (INSIDE || (row < a.rows && col < padded)) {
             T::store_row_codes(a.data + (size_t)row * (padded / 2) + col / 2, codes);
             if ((lane & (4 * T::kLanes - 1)) == 0) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = four;
         }
     }
 }
 
-// Down the columns, and along the rows too where wanted, in one pass: a wave holds 32 rows of 64 lanes' columns in registers, so that a
-// column's block is one lane's and a row's is kLanes'.  Four waves of a block take 128 rows, whose scales are one dword a column.
-template <typename T, bool ROWS>
-__global__ __launch_bounds__(256) void quantize_both_kernel(const QuantizeArgs a) {
-    constexpr int R = 32;
-    __shared__ uint8_t bytes_t[64 * T::kPer * 4];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t chunk = blockIdx.x % a.chunks, band = blockIdx.x / a.chunks, row0 = band * 128 + wave * R;
-    const uint32_t col = (chunk * 64 + lane) * T::kPer, padded = (a.cols + 127u) & ~127u;
+template <typename T, int R, bool ONCE>
+__global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a) {
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+    const uint32_t band = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - band * a.chunks, row0 = (band * 4 + wave) * R;
+    const uint32_t col = (chunk * 64 + lane) * T::kPer;
+    if ((chunk + 1) * 64 * T::kPer <= a.cols && row0 + R <= a.rows) quantize_rows<T, R, ONCE, true>(a, lane, row0, col);
+    else quantize_rows<T, R, ONCE, false>(a, lane, row0, col);
+}
+
+// Down the columns, and along the rows too where wanted, in one pass.  A wave holds R rows of 64 lanes' columns in registers, so that R of a
+// column's block are one lane's; 32 / R waves share a block and exchange its largest magnitudes.  A block's waves take 128 rows, of which a column's codes are 64
+// bytes: they go through LDS, so that they leave as such (straight from the lanes they would be a few bytes here and there).
+constexpr int kBothRows = 16, kBothWaves = 128 / kBothRows;
+
+template <typename T>
+struct BothShared {
+    uint8_t codes[64 * T::kPer * kGroupBytes];
+    u32x4 largest[kBothWaves][64];
+    uint32_t scales[64 * T::kPer];
+};
+
+template <typename T, bool ROWS, bool ONCE, bool INSIDE>
+__device__ __forceinline__ void quantize_both(const QuantizeArgs &a, BothShared<T> &shared, uint32_t lane, uint32_t wave, uint32_t row0, uint32_t col) {
+    constexpr int R = kBothRows, kShare = 32 / R;
+    constexpr uint32_t kPiece = R / 2, kPlaces = kGroupBytes / kPiece;
+    const uint32_t padded = (a.cols + 127u) & ~127u;
     u32x4 v[R];
+    load_rows<T, R, INSIDE, ONCE>(v, a, row0, col);
+    u32x4 m = T::magnitudes(v[0]);
 #pragma unroll
-    for (int r = 0; r < R; ++r) v[r] = load_part<T>(a, row0 + r, col);
+    for (int r = 1; r < R; ++r) m = T::larger(m, T::magnitudes(v[r]));
+    shared.largest[wave][lane] = m;
     if constexpr (ROWS) {
         constexpr uint32_t kGroupLanes = 4 * T::kLanes;        // whose blocks share a dword: 32 or 16
-        uint32_t kept[R / kGroupLanes] = {};
+        uint32_t kept = 0;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint32_t byte = scale_byte(T::row_max(T::magnitudes(v[r])));
             const uint32_t codes = T::row_codes(v[r], scale_of(byte)), four = T::gather_bytes(byte, lane);
             const uint32_t row = row0 + r;
-            if (row < a.rows && col < padded) T::store_row_codes(a.data + (size_t)row * (padded / 2) + col / 2, codes);
+            if (INSIDE || (row < a.rows && col < padded)) T::store_row_codes(a.data + (size_t)row * (padded / 2) + col / 2, codes);
             // lane r of the group keeps row r's, so that they leave side by side
-            if ((lane & (kGroupLanes - 1)) == r % kGroupLanes) kept[r / kGroupLanes] = four;
+            if ((lane & (kGroupLanes - 1)) == (uint32_t)r) kept = four;
         }
-#pragma unroll
-        for (uint32_t k = 0; k < R / kGroupLanes; ++k) {
-            const uint32_t row = row0 + k * kGroupLanes + (lane & (kGroupLanes - 1));
-            if (row < a.rows && col < padded) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = kept[k];
-        }
+        const uint32_t row = row0 + (lane & (kGroupLanes - 1));
+        if ((lane & (kGroupLanes - 1)) < R && (INSIDE || (row < a.rows && col < padded))) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = kept;
     }
-    u32x4 m = T::magnitudes(v[0]);
+    __syncthreads();
 #pragma unroll
-    for (int r = 1; r < R; ++r) m = T::larger(m, T::magnitudes(v[r]));
-    const size_t padded_rows = ((size_t)a.rows + 127) & ~(size_t)127;
+    for (int k = 0; k < kShare; ++k) m = T::larger(m, shared.largest[(wave & ~(uint32_t)(kShare - 1)) + k][lane]);
 #pragma unroll
     for (int c = 0; c < (int)T::kPer; ++c) {
         const uint32_t byte = scale_byte(T::pick(m, c));
         const float scale = scale_of(byte);
-        u32x4 codes;
+        const uint32_t column = lane * T::kPer + c;
+        // piece w of a column at place w ^ lane, for the banks' sake
+        uint32_t *to = reinterpret_cast<uint32_t *>(shared.codes + column * kGroupBytes + ((wave ^ (lane & (kPlaces - 1))) * kPiece));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) codes[k] = T::column_codes(v + 8 * k, c, scale);
-        if (col + c < a.cols) *reinterpret_cast<u32x4 *>(a.data_t + (size_t)(col + c) * (padded_rows / 2) + row0 / 2) = codes;
-        bytes_t[(lane * T::kPer + c) * 4 + wave] = (uint8_t)byte;
+        for (int k = 0; k < R / 8; ++k) to[k] = T::column_codes(v + 8 * k, c, scale);
+        if (wave % kShare == 0) reinterpret_cast<uint8_t *>(&shared.scales[column])[wave / kShare] = (uint8_t)byte;
     }
+}
+
+template <typename T, bool ROWS, bool ONCE>
+__global__ __launch_bounds__(64 * kBothWaves, 4) void quantize_both_kernel(const QuantizeArgs a) {
+    constexpr uint32_t kColumns = 64 * T::kPer, kThreads = 64 * kBothWaves, kPiece = kBothRows / 2, kPlaces = kGroupBytes / kPiece;
+    __shared__ BothShared<T> shared;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+    const uint32_t band = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - band * a.chunks, row0 = band * 128 + wave * kBothRows;
+    const uint32_t first = chunk * kColumns, col = first + lane * T::kPer;
+    if (first + kColumns <= a.cols && band * 128 + 128 <= a.rows) quantize_both<T, ROWS, ONCE, true>(a, shared, lane, wave, row0, col);
+    else quantize_both<T, ROWS, ONCE, false>(a, shared, lane, wave, row0, col);
     __syncthreads();
-    const uint32_t *fours = reinterpret_cast<const uint32_t *>(bytes_t);
-    for (uint32_t c = threadIdx.x; c < 64 * T::kPer; c += 256) {
-        const uint32_t to = chunk * 64 * T::kPer + c;
-        if (to < a.cols) a.scales_t[(size_t)band * a.cols + to] = fours[c];
+    const size_t row_bytes = (((size_t)a.rows + 127) & ~(size_t)127) / 2;
+#pragma unroll
+    for (uint32_t i = threadIdx.x; i < kColumns * 4; i += kThreads) {
+        const uint32_t column = i >> 2, part = i & 3u, mixed = column / T::kPer & (kPlaces - 1);
+        if (first + column >= a.cols) continue;
+        const uint8_t *codes = shared.codes + column * kGroupBytes;
+        u32x4 v;
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k)
+            v[k] = *reinterpret_cast<const uint32_t *>(codes + (((part * 16 + k * 4) / kPiece) ^ mixed) * kPiece + (k * 4) % kPiece);
+        *reinterpret_cast<u32x4 *>(a.data_t + (size_t)(first + column) * row_bytes + band * kGroupBytes + part * 16) = v;
     }
+    if (threadIdx.x < kColumns && first + threadIdx.x < a.cols) a.scales_t[(size_t)band * a.cols + first + threadIdx.x] = shared.scales[threadIdx.x];
 }
 
 // ---------------------------------------------------------- dequantise ----
@@ -250,11 +332,11 @@ struct DequantizeArgs {
     uint32_t chunks;           // of 512 columns
 };
 
-// A lane takes eight codes, a wave R rows of 512 columns.
+// A lane takes eight codes, a wave R rows of 512 columns.  Stored with nt: 8192 x 8192 bf16 25.0 us (6.8 TB/s) against 33.4.
 template <bool OUT_BF16, int R>
 __global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs a) {
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6;
-    const uint32_t chunk = blockIdx.x % a.chunks, row0 = (blockIdx.x / a.chunks * 4 + wave) * R;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+    const uint32_t band = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - band * a.chunks, row0 = (band * 4 + wave) * R;
     const uint32_t col = (chunk * 64 + lane) * 8, padded = (a.cols + 127u) & ~127u;
     if (col >= a.cols) return;
     uint32_t codes[R], bytes[R];
@@ -282,7 +364,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs a)
             o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[r], scale, 3));
             if (nan) o = u32x4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u};
             uint16_t *to = static_cast<uint16_t *>(a.out) + at;
-            if (col + 8 <= a.cols) *reinterpret_cast<u32x4_bf16 *>(to) = o;
+            if (col + 8 <= a.cols) __builtin_nontemporal_store(o, reinterpret_cast<u32x4_bf16 *>(to));
             else
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
@@ -298,8 +380,8 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs a)
             for (int k = 0; k < 8; ++k) o[k >> 2][k & 3] = nan ? 0x7FC00000u : __float_as_uint(p[k >> 1][k & 1]);
             uint32_t *to = static_cast<uint32_t *>(a.out) + at;
             if (col + 8 <= a.cols) {
-                reinterpret_cast<u32x4_f32 *>(to)[0] = o[0];
-                reinterpret_cast<u32x4_f32 *>(to)[1] = o[1];
+                __builtin_nontemporal_store(o[0], reinterpret_cast<u32x4_f32 *>(to));
+                __builtin_nontemporal_store(o[1], reinterpret_cast<u32x4_f32 *>(to) + 1);
             } else {
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
@@ -343,9 +425,6 @@ struct TilesArgs {
     uint32_t tiles_m, tiles_n;
     uint32_t splits;
 };
-
-// a value that all lanes have, for the scalar unit
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
 
 // all but the last N loads of this wave are there (neither a barrier nor a read waits for loads into LDS by itself), and so is what it read from LDS
 template <int N>
