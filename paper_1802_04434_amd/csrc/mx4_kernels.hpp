@@ -53,6 +53,11 @@ __device__ __forceinline__ uint32_t dpp_xor2(uint32_t v) { return (uint32_t)__bu
 __device__ __forceinline__ uint32_t dpp_mirror8(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141 /* row_half_mirror */, 0xF, 0xF, false); }
 __device__ __forceinline__ uint32_t dpp_mirror16(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140 /* row_mirror */, 0xF, 0xF, false); }
 
+// lane SEL of each four, for each of them; the lane N further on of 16
+template <int SEL>
+__device__ __forceinline__ uint32_t dpp_quad(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, SEL /* quad_perm */, 0xF, 0xF, false); }
+template <int N>
+__device__ __forceinline__ uint32_t dpp_turn(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x120 + N /* row_ror */, 0xF, 0xF, false); }
 __device__ __forceinline__ uint32_t umax(uint32_t a, uint32_t b) { return a > b ? a : b; }
 __device__ __forceinline__ uint32_t pk_umax16(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
@@ -84,6 +89,17 @@ struct F32 {
     }
     // bits of element c's magnitude, as an fp32
     static __device__ __forceinline__ uint32_t pick(u32x4 m, int c) { return m[c]; }
+    // bits of the largest of 32 in four rows, in all of their lanes
+    static __device__ __forceinline__ void four_max(const u32x4 (&v)[4], uint32_t (&bits)[4]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) bits[i] = row_max(magnitudes(v[i]));
+    }
+    // of lanes k, k + 8, k + 16 and k + 24 the bytes as a dword
+    static __device__ __forceinline__ uint32_t gather_four(uint32_t byte, uint32_t lane) {
+        uint32_t v = byte << ((lane >> 3 & 3u) * 8);
+        v |= dpp_turn<8>(v);
+        return v | (uint32_t)__shfl_xor((int)v, 16);
+    }
     static __device__ __forceinline__ uint32_t row_codes(u32x4 v, float scale) {
         uint32_t o = 0;
         o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[0]), __uint_as_float(v[1]), scale, 0);
@@ -134,6 +150,29 @@ struct Bf16 {
         return umax(v << 16, v & 0xFFFF0000u);
     }
     static __device__ __forceinline__ uint32_t pick(u32x4 m, int c) { return c & 1 ? m[c >> 1] & 0xFFFF0000u : m[c >> 1] << 16; }
+    static __device__ __forceinline__ void four_max(const u32x4 (&v)[4], uint32_t (&bits)[4]) {
+        uint32_t m[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32x4 e = magnitudes(v[i]);
+            m[i] = pk_umax16(pk_umax16(e[0], e[1]), pk_umax16(e[2], e[3]));
+        }
+        // two rows side by side
+#pragma unroll
+        for (int i = 0; i < 4; i += 2) {
+            uint32_t two = pk_umax16(__builtin_amdgcn_perm(m[i + 1], m[i], 0x05040100u), __builtin_amdgcn_perm(m[i + 1], m[i], 0x07060302u));
+            two = pk_umax16(two, dpp_xor1(two));
+            two = pk_umax16(two, dpp_xor2(two));
+            bits[i] = two << 16;
+            bits[i + 1] = two & 0xFFFF0000u;
+        }
+    }
+    // of lanes k, k + 4, k + 8 and k + 12 the bytes as a dword
+    static __device__ __forceinline__ uint32_t gather_four(uint32_t byte, uint32_t lane) {
+        uint32_t v = byte << ((lane >> 2 & 3u) * 8);
+        v |= dpp_turn<4>(v);
+        return v | dpp_turn<8>(v);
+    }
     static __device__ __forceinline__ bf16x2 pair(uint32_t v) { return __builtin_bit_cast(bf16x2, v); }
     static __device__ __forceinline__ uint32_t row_codes(u32x4 v, float scale) {
         uint32_t o = 0;
@@ -395,14 +434,6 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs a)
 
 __device__ __forceinline__ i32x8 widened(u32x4 v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
 
-// four steps of 128: block k of each lane's four, scaled by byte k of its dword (format 4: E2M1)
-__device__ __forceinline__ f32x4 multiply_16(const u32x4 *a, uint32_t sa, const u32x4 *b, uint32_t sb, f32x4 c) {
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[0]), widened(b[0]), c, 4, 4, 0, (int)sa, 0, (int)sb);
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[1]), widened(b[1]), c, 4, 4, 1, (int)sa, 1, (int)sb);
-    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[2]), widened(b[2]), c, 4, 4, 2, (int)sa, 2, (int)sb);
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(a[3]), widened(b[3]), c, 4, 4, 3, (int)sa, 3, (int)sb);
-}
-
 template <bool OUT_BF16>
 __device__ __forceinline__ void store_out(void *out, size_t at, float v) {
     if constexpr (OUT_BF16) static_cast<__bf16 *>(out)[at] = (__bf16)v;
@@ -619,23 +650,10 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
 }
 
 // ------------------------------------------------- product of a few rows ----
-
-// the 64 bytes and the scales of one row and group; zeros beyond the matrix
-struct Part {
-    u32x4 v[4];
-    uint32_t s;
-    __device__ __forceinline__ void load(const uint8_t *data, const uint32_t *scales, uint32_t row, uint32_t rows, uint32_t group, uint32_t groups) {
-        s = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = u32x4{0, 0, 0, 0};
-        if (row >= rows || group >= groups) return;
-        const u32x4 *p = reinterpret_cast<const u32x4 *>(data + ((size_t)row * groups + group) * kGroupBytes);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = p[k];
-        s = scales[(size_t)group * rows + row];
-    }
-};
-
+// Up to 16 rows of x, quantised on the way.  A wave streams 16 rows of w, or SPLIT of a block's waves share them, each with every SPLIT-th step of 512
+// columns, and their sums are added through LDS in order.  A block first brings x in MX4 into LDS, or as many steps of it as fit, while its waves' first steps of w are on
+// the way.  What has to be read is w, and that is what bounds it: its steps go straight into LDS, each wave's into a ring of its own, so that a load
+// takes 256 bytes of a row and many are on the way.
 
 struct LinearArgs {
     const void *x;
@@ -645,67 +663,170 @@ struct LinearArgs {
     size_t ldx, ldo;
     uint32_t T, N, K, groups;
     uint32_t first;            // row of w that the launch begins with
+    uint32_t log_split;
 };
 
-// One row's group of x in MX4, in one lane: its 128 columns as 32-column blocks, each quantised by itself.
-template <typename T>
-__device__ __forceinline__ void quantize_group(const LinearArgs &a, uint32_t row, uint32_t group, u32x4 *codes, uint32_t &scales) {
-    constexpr int kVecs = kBlockCols / T::kPer;
-    scales = 0;
+constexpr int kLinearWaves = 8;
+constexpr uint32_t kLinearGroups = 4, kLinearCodeBytes = 16 * kLinearGroups * kGroupBytes, kLinearStepBytes = kLinearCodeBytes + 16 * kLinearGroups * 4;     // a step of 16 rows: codes, scales
+
+// STEPS of x in LDS, DEPTH of w for each wave
+template <int STEPS, int DEPTH>
+struct LinearShared {
+    u32x4 codes[STEPS][kLinearGroups * 4][16];
+    uint32_t scales[STEPS][64];
+    __attribute__((aligned(128))) char w[kLinearWaves][DEPTH][kLinearStepBytes];
+};
+
+// Brings rows of x, four parts of 64 lanes' columns at once, the next ones on the way; `then` after the first ones.  Every block does it, so it is kept short:
+// a lane of four finds one part's scale for all of them, and the loop is not unrolled, since its first pass waits for the instructions themselves.
+template <typename T, int STEPS, int DEPTH, typename F>
+__device__ __forceinline__ void bring_x(LinearShared<STEPS, DEPTH> &shared, const LinearArgs &a, uint32_t base, uint32_t steps, uint32_t lane, uint32_t wave, F then) {
+    constexpr uint32_t kWidth = 64 * T::kPer, kStep = kLinearGroups * kGroupCols, kParts = kStep / kWidth;
+    const uint32_t fours = (steps * kParts + 3) / 4;
+    struct Item {
+        uint32_t token, four;
+    };
+    auto load = [&](u32x4 (&v)[4], Item at) {
+        const typename T::elem *x = static_cast<const typename T::elem *>(a.x) + (size_t)at.token * a.ldx;
+        const uint32_t col = base * kStep + at.four * 4 * kWidth + lane * T::kPer, last = a.K - T::kPer;
+        // where x ends a lane loads what ends with it
 #pragma unroll
-    for (int k = 0; k < 4; ++k) codes[k] = u32x4{0, 0, 0, 0};
-    if (row >= a.T || group >= a.groups) return;
-    QuantizeArgs part{};
-    part.x = a.x;
-    part.ld = a.ldx;
-    part.rows = a.T;
-    part.cols = a.K;
+        for (uint32_t i = 0; i < 4; ++i) v[i] = T::load(x + (col + i * kWidth < last ? col + i * kWidth : last));
+    };
+    auto put = [&](const u32x4 (&v)[4], Item at) {
+        uint32_t bits[4];
+        T::four_max(v, bits);
+        const uint32_t mine = lane & 2u ? (lane & 1u ? bits[3] : bits[2]) : (lane & 1u ? bits[1] : bits[0]), byte = scale_byte(mine);
+        const uint32_t scale = __float_as_uint(scale_of(byte));
+        const float scales[4] = {__uint_as_float(dpp_quad<0x00>(scale)), __uint_as_float(dpp_quad<0x55>(scale)), __uint_as_float(dpp_quad<0xAA>(scale)),
+                                 __uint_as_float(dpp_quad<0xFF>(scale))};
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        u32x4 v[kVecs];
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) v[i] = load_part<T>(part, row, group * kGroupCols + k * kBlockCols + i * T::kPer);
-        u32x4 m = T::magnitudes(v[0]);
-#pragma unroll
-        for (int i = 1; i < kVecs; ++i) m = T::larger(m, T::magnitudes(v[i]));
-        uint32_t bits = T::pick(m, 0);
-#pragma unroll
-        for (int c = 1; c < (int)T::kPer; ++c) bits = umax(bits, T::pick(m, c));
-        const uint32_t byte = scale_byte(bits);
-        const float scale = scale_of(byte);
-        scales |= byte << (8 * k);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-            const uint32_t c = T::row_codes(v[i], scale);
-            if constexpr (T::kPer == 8) codes[k][i] = c;
-            else codes[k][i / 2] |= c << (16 * (i & 1));
+        for (uint32_t i = 0; i < 4; ++i) {
+            const uint32_t part = at.four * 4 + i, block = (i % kParts) * (kWidth / kBlockCols) + lane / T::kLanes;
+            // rows are mixed, so that a row's blocks lie in different banks
+            uint8_t *to = reinterpret_cast<uint8_t *>(&shared.codes[part / kParts][block][at.token ^ block]);
+            T::store_row_codes(to + (lane & (T::kLanes - 1)) * (T::kPer / 2), T::row_codes(v[i], scales[i]));
         }
+        const uint32_t dword = T::gather_four(byte, lane), part = at.four * 4 + (lane & 3u), group = part % kParts * (kWidth / kGroupCols) + lane / (4 * T::kLanes);
+        if ((lane & (4 * T::kLanes - 1)) < 4) shared.scales[part / kParts][group * 16 + at.token] = dword;
+    };
+    const uint32_t more = uniform(kLinearWaves / fours), rest = kLinearWaves - more * fours;
+    auto advance = [&](Item &i) {
+        i.token += more, i.four += rest;
+        if (i.four >= fours) i.four -= fours, ++i.token;
+    };
+    Item at;
+    at.token = uniform(wave / fours);
+    at.four = wave - at.token * fours;
+    if (a.K < T::kPer) {
+        then();
+        QuantizeArgs m{};
+        m.x = a.x;
+        m.ld = a.ldx;
+        m.rows = a.T;
+        m.cols = a.K;
+        for (; at.token < a.T; advance(at)) {
+            u32x4 v[4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) v[i] = load_part<T>(m, at.token, (at.four * 4 + i) * kWidth + lane * T::kPer);
+            put(v, at);
+        }
+        return;
+    }
+    u32x4 v[4];
+    if (at.token < a.T) load(v, at);
+    then();
+    while (at.token < a.T) {
+        const uint32_t first = base * kStep + at.four * 4 * kWidth;
+        if (first + 4 * kWidth > a.K) {
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t col = first + i * kWidth + lane * T::kPer, over = col + T::kPer <= a.K ? 0 : col - (a.K - T::kPer);
+                if (a.K % T::kPer) v[i] = T::drop(v[i], over);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[i][k] = over >= T::kPer ? 0u : v[i][k];
+            }
+        }
+        const Item now = at;
+        advance(at);
+        put(v, now);
+        if (at.token < a.T) load(v, at);
     }
 }
 
-constexpr int kLinearWaves = 8;
-
-// A block takes 16 rows of w, its waves a share of the columns each; their sums are added through LDS in order.
-template <typename T, bool OUT_BF16>
+template <typename T, bool OUT_BF16, bool ONCE, int STEPS, int DEPTH>
 __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearArgs a) {
-    __shared__ f32x4 part[kLinearWaves][64];
-    const uint32_t lane = threadIdx.x & 63u, wave = threadIdx.x >> 6, r = lane & 15u, q = lane >> 4;
-    const uint32_t n0 = a.first + blockIdx.x * 16;
-    const uint32_t steps = (a.groups + 3) / 4, from = steps * wave / kLinearWaves, to = steps * (wave + 1) / kLinearWaves;
-    f32x4 c = {0, 0, 0, 0};
-    for (uint32_t s = from; s < to; ++s) {
-        Part w;
-        u32x4 x[4];
-        uint32_t sx;
-        w.load(a.w, a.sw, n0 + r, a.N, 4 * s + q, a.groups);
-        quantize_group<T>(a, r, 4 * s + q, x, sx);
-        c = multiply_16(x, sx, w.v, w.s, c);
-    }
-    part[wave][lane] = c;
-    __syncthreads();
-    if (wave) return;
+    __shared__ LinearShared<STEPS, DEPTH> shared;
+    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), r = lane & 15u, q = lane >> 4;
+    const uint32_t split = 1u << a.log_split, share = wave & (split - 1);
+    const uint32_t n0 = a.first + (blockIdx.x * (kLinearWaves >> a.log_split) + (wave >> a.log_split)) * 16;
+    const uint32_t steps = (a.groups + kLinearGroups - 1) / kLinearGroups, mine = steps > share ? (steps - share + split - 1) >> a.log_split : 0;
+    const uint32_t row_bytes = a.groups * kGroupBytes;
+    // Rows beyond w read as zero.  Groups beyond the last are the next row's codes, with scales that read as zero; x's codes are zero there.
+    const uint32_t rows = n0 < a.N ? (a.N - n0 < 16 ? a.N - n0 : 16) : 0;
+    const ss::Window ww = ss::window(a.w, (size_t)(rows ? n0 : 0) * row_bytes, rows * row_bytes);
+    const ss::Window ws = ss::window(a.sw, 0, a.groups * a.N * 4);
+    typedef __attribute__((address_space(3))) void *Lds;
+    uint32_t from[4];       // 16 lanes take 256 bytes of a row, chunk c of row r to place c ^ r
 #pragma unroll
-    for (int k = 1; k < kLinearWaves; ++k) c += part[k][lane];
+    for (uint32_t i = 0; i < 4; ++i) from[i] = (4 * i + q) * row_bytes + ((r ^ (4 * i + q)) * 16);
+    const uint32_t from_s = (q * a.N + (n0 + r < a.N ? n0 + r : a.N - 1)) * 4;
+    // Rows that begin a power of two apart begin in the same memory channels: each wave begins at another of its steps
+    const uint32_t per = STEPS >> a.log_split, tile = n0 / 16, tail = mine & (per - 1), turn = tile & (per - 1), turn_tail = tail ? uniform(tile % tail) : 0;
+    auto step_of = [&](uint32_t k) {
+        k = k < mine ? k : mine - 1;
+        const uint32_t base = k & ~(per - 1), left = mine - base < per ? tail : per;
+        uint32_t i = k - base + (mine - base < per ? turn_tail : turn);
+        if (i >= left) i -= left;
+        return ((base + i) << a.log_split) + share;
+    };
+    auto fetch = [&](uint32_t place, uint32_t k) {
+        const uint32_t step = mine ? step_of(k) : 0;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ww, (Lds)(shared.w[wave][place] + i * 1024), 16, (int)from[i], (int)(step * (kLinearGroups * kGroupBytes)), 0, ONCE ? 2 : 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ws, (Lds)(shared.w[wave][place] + kLinearCodeBytes), 4, (int)from_s, (int)(step * kLinearGroups * a.N * 4), 0, 0);
+    };
+    f32x4 c = {0, 0, 0, 0};
+    uint32_t k = 0, place = 0;
+    for (uint32_t base = 0; base < steps; base += STEPS) {
+        const uint32_t count = steps - base < STEPS ? steps - base : STEPS;
+        if (base) __syncthreads();
+        auto start = [&] {
+            if (base) return;
+#pragma unroll
+            for (int i = 0; i < DEPTH; ++i) fetch((uint32_t)i, (uint32_t)i);
+        };
+        bring_x<T>(shared, a, base, count, lane, wave, start);
+        __syncthreads();
+        const uint32_t end = mine < ((base + STEPS) >> a.log_split) ? mine : (base + STEPS) >> a.log_split;
+        for (; k < end; ++k) {
+                arrived<5 * (DEPTH - 1)>();
+                u32x4 f[4], g[4];
+                const uint32_t at = step_of(k) - base;
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j) {
+                    g[j] = *reinterpret_cast<const u32x4 *>(shared.w[wave][place] + r * 256 + (((q * 4 + j) ^ r) * 16));
+                    f[j] = shared.codes[at][q * 4 + j][r ^ (q * 4 + j)];
+                }
+                const uint32_t sx = shared.scales[at][lane], sn = reinterpret_cast<const uint32_t *>(shared.w[wave][place] + kLinearCodeBytes)[lane];
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                fetch(place, k + DEPTH);
+                place = place + 1 < DEPTH ? place + 1 : 0;
+                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[0]), widened(g[0]), c, 4, 4, 0, (int)sx, 0, (int)sn);
+                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[1]), widened(g[1]), c, 4, 4, 1, (int)sx, 1, (int)sn);
+                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[2]), widened(g[2]), c, 4, 4, 2, (int)sx, 2, (int)sn);
+                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[3]), widened(g[3]), c, 4, 4, 3, (int)sx, 3, (int)sn);
+        }
+    }
+    arrived<0>();       // nothing is on its way into LDS that others may have
+    if (split > 1) {
+        f32x4 *part = reinterpret_cast<f32x4 *>(shared.w[wave][0]);
+        part[lane] = c;
+        __syncthreads();
+        if (share) return;
+        for (uint32_t i = 1; i < split; ++i) c += reinterpret_cast<const f32x4 *>(shared.w[wave + i][0])[lane];
+    }
     const uint32_t n = n0 + r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
