@@ -48,7 +48,23 @@ auto linear_kernel(size_t steps, bool once) {
 template <typename T>
 auto linear_kernel(ss_dtype odt, size_t steps, bool once) { return odt == SS_BF16 ? linear_kernel<T, true>(steps, once) : linear_kernel<T, false>(steps, once); }
 
-// How a product, or a part of one, is cut: tiles of 64 times `tile` squared, and the sum over the columns into `splits` parts
+inline int few_rows(decltype(linear_kernel<mx4::F32>) *kernels, ss_dtype odt, mx4::LinearArgs a, hipStream_t stream) {
+    const size_t tiles = ((size_t)a.N + 15) / 16, steps = ((size_t)a.groups + mx4::kLinearGroups - 1) / mx4::kLinearGroups;
+    // as few waves to the same rows as fill the card: each block brings x
+    while (2u << a.log_split <= mx4::kLinearWaves && (tiles << a.log_split) < kLinearBlocks * mx4::kLinearWaves && (size_t)1 << a.log_split < steps) ++a.log_split;
+    const auto kernel = kernels(odt, steps, (size_t)a.N * a.groups * mx4::kGroupBytes >= kLinearOnce);
+    constexpr int kThreads = 64 * mx4::kLinearWaves;
+    const size_t rows = 16 * (mx4::kLinearWaves >> a.log_split), most = kMaxThreads / kThreads;
+    for (size_t first = 0; first < a.N; first += most * rows) {
+        a.first = (uint32_t)first;
+        const int rc = launch(kernel, std::min((a.N - first + rows - 1) / rows, most), 0, stream, a, kThreads);
+        if (rc != SS_OK) return rc;
+    }
+    return SS_OK;
+}
+
+// How a product, or a part of one, is cut: tiles of 64 times `tile` squared (0: a few rows or columns of the result, by the kernel for them), and the sum over the
+// columns into `splits` parts
 struct Plan {
     int tile;
     size_t splits;
@@ -82,8 +98,18 @@ inline Plan plan_of(size_t M, size_t N, size_t K, bool may_split) {
             if (us < best.us) best = Plan{s.tile, splits, us};
         }
     }
+    // The few rows' kernel: w's bytes, and what it costs to bring each 8,192 columns of x; tiles have to read w too.  us, few rows / tiles: 1 x 4096 x 4096 4.0 / 8.2, 16 x 8192 x
+    // 4096 6.2 / 9.6, 16 x 16384 x 16384 28.2 / 31.7, but 16 x 16 x 32768, of which tiles can split the sum, 12.0 / 7.9
+    if (std::min(M, N) <= SS_MX4_LINEAR_MAX_ROWS) {
+        const double bytes = (double)std::max(M, N) * groups_of(K) * 68, us = 2.0 + bytes / 6.5e6 + 2.6 * (double)((groups_of(K) - 1) / 64);
+        if (us < std::max(best.us, 3.0 + bytes / 4.6e6)) best = Plan{0, 1, us};
+    }
     return best;
 }
+
+// A result that the memory-side cache can hold stays there.  us, left to the L2 / sent on / with nt: 4096 x 4096 x 4096 in bf16 (33 MB) 37.2 / 35.7 / 36.0, in fp32 41.7 / 40.1 /
+// 41.1, 4096 x 8192 x 2048 in bf16 (67 MB) 50.0 / 45.8 / 47.5, in fp32 68.0 / 69.5 / 65.1, 8192 x 12288 x 1024 in fp32 (403 MB) 158 / 134 / 111.
+constexpr size_t kProductKeeps = (size_t)1 << 27;
 
 // A part of the result with a plan of its own
 struct Part {
@@ -213,10 +239,23 @@ int ss_mx4_matmul(const uint8_t *a_data, const uint8_t *a_scales, const uint8_t 
         const int tile = part.plan.tile;
         const bool join = part.plan.splits > 1, bf16 = odt == SS_BF16 && !join;
         void *to = static_cast<char *>(out) + (part.m * ld + part.n) * grad_bytes(odt);
+        if (tile == 0) {
+            const bool wide = part.M <= part.N;       // a's rows are the few, or b's
+            const uint8_t *data[2] = {a_data + part.m * groups * mx4::kGroupBytes, b_data + part.n * groups * mx4::kGroupBytes};
+            const uint32_t *scales[2] = {reinterpret_cast<const uint32_t *>(a_scales) + part.m, reinterpret_cast<const uint32_t *>(b_scales) + part.n};
+            const uint32_t rows[2] = {(uint32_t)M, (uint32_t)N};
+            const int rc = few_rows(linear_kernel<mx4::Codes>, odt,
+                                    {data[!wide], scales[!wide], data[wide], scales[wide], to, 0, wide ? ld : 1, wide ? 1 : ld, (uint32_t)std::min(part.M, part.N),
+                                     (uint32_t)std::max(part.M, part.N), (uint32_t)K, (uint32_t)groups, rows[!wide], rows[wide], 0, 0},
+                                    stream);
+            if (rc != SS_OK) return rc;
+            continue;
+        }
         mx4::TilesArgs a{a_data + part.m * groups * mx4::kGroupBytes, b_data + part.n * groups * mx4::kGroupBytes,
                          reinterpret_cast<const uint32_t *>(a_scales) + part.m, reinterpret_cast<const uint32_t *>(b_scales) + part.n,
                          join ? scratch : to, join ? part.N : ld, (uint32_t)part.M, (uint32_t)part.N, (uint32_t)M, (uint32_t)N, (uint32_t)groups,
-                         (uint32_t)tiles_of(part.M, tile), (uint32_t)tiles_of(part.N, tile), (uint32_t)part.plan.splits};
+                         (uint32_t)tiles_of(part.M, tile), (uint32_t)tiles_of(part.N, tile), (uint32_t)part.plan.splits,
+                         join || M * N * grad_bytes(odt) < kProductKeeps};
         const auto kernel = tile == 4 ? (bf16 ? mx4::matmul_tiles_kernel<true, 4> : mx4::matmul_tiles_kernel<false, 4>)
                             : tile == 2 ? (bf16 ? mx4::matmul_tiles_kernel<true, 2> : mx4::matmul_tiles_kernel<false, 2>)
                                         : (bf16 ? mx4::matmul_tiles_kernel<true, 1> : mx4::matmul_tiles_kernel<false, 1>);
@@ -241,23 +280,10 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
     Span spans[4] = {matrix(x, T, K, ldx, xdt, false), span(w_data, ss_mx4_data_bytes(N, K), false),
                      span(w_scales, ss_mx4_scale_bytes(N, K), false), matrix(out, T, N, ldo, odt, true)};
     if (written_spans_overlap(spans, 4)) return SS_ERR_ARG;
-    const size_t tiles = (N + 15) / 16, steps = (groups_of(K) + mx4::kLinearGroups - 1) / mx4::kLinearGroups;
-    // as few waves to the same rows as fill the card: each block quantises x
-    uint32_t log_split = 0;
-    while (2u << log_split <= mx4::kLinearWaves && (tiles << log_split) < kLinearBlocks * mx4::kLinearWaves && (size_t)1 << log_split < steps) ++log_split;
-    mx4::LinearArgs a{x, w_data, reinterpret_cast<const uint32_t *>(w_scales), out, ldx, ldo, (uint32_t)T, (uint32_t)N, (uint32_t)K,
-                      (uint32_t)groups_of(K), 0, log_split};
-    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-    constexpr int kThreads = 64 * mx4::kLinearWaves;
-    const bool once = ss_mx4_data_bytes(N, K) >= kLinearOnce;
-    const auto kernel = xdt == SS_BF16 ? linear_kernel<mx4::Bf16>(odt, steps, once) : linear_kernel<mx4::F32>(odt, steps, once);
-    const size_t rows = 16 * (mx4::kLinearWaves >> log_split), most = kMaxThreads / kThreads;
-    for (size_t first = 0; first < N; first += most * rows) {
-        a.first = (uint32_t)first;
-        const int rc = launch(kernel, std::min((N - first + rows - 1) / rows, most), 0, stream, a, kThreads);
-        if (rc != SS_OK) return rc;
-    }
-    return SS_OK;
+    return few_rows(xdt == SS_BF16 ? linear_kernel<mx4::Bf16> : linear_kernel<mx4::F32>, odt,
+                    {x, nullptr, w_data, reinterpret_cast<const uint32_t *>(w_scales), out, ldx, ldo, 1, (uint32_t)T, (uint32_t)N, (uint32_t)K, (uint32_t)groups_of(K), 0,
+                     (uint32_t)N, 0, 0},
+                    static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"

@@ -22,6 +22,8 @@ typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 // plain matrices are aligned to their element alone
@@ -455,24 +457,30 @@ struct TilesArgs {
     uint32_t groups;           // of 128 columns
     uint32_t tiles_m, tiles_n;
     uint32_t splits;
+    bool kept;                 // the result, in the memory-side cache
 };
 
 // all but the last N loads of this wave are there (neither a barrier nor a read waits for loads into LDS by itself), and so is what it read from LDS
 template <int N>
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
+// 16 bytes at any alignment, sent on by the L2 at once: what is left there is sent when the kernel ends, with nothing beside it.  The next instruction may change v only
+// when the store has read it.
+__device__ __forceinline__ void store_through(void *p, u32x4 v) { asm volatile("global_store_dwordx4 %0, %1, off sc1\n\ts_nop 1" ::"v"(p), "v"(v) : "memory"); }
+
 template <int T>
 struct Fragments {
     u32x4 a[T], b[T];
 };
 
-// part of 2 T of the multiplications of a quarter; BYTE: which one, and of the scales' bytes
+// part of 2 T of the multiplications of a quarter; BYTE: which one, and of the scales' bytes.  b is the first operand, so that a lane has four
+// neighbours of a row of the result.
 template <int BYTE, int T>
 __device__ __forceinline__ void multiply(f32x16 (&c)[T][T], const Fragments<T> &f, const uint32_t (&s)[2 * T], int part) {
 #pragma unroll
     for (int x = part * T / 2; x < (part + 1) * T / 2; ++x)
-        c[x / T][x % T] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(f.a[x / T]), widened(f.b[x % T]), c[x / T][x % T], 4, 4, BYTE, (int)s[x / T],
-                                                                          BYTE, (int)s[T + x % T]);
+        c[x / T][x % T] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(widened(f.b[x % T]), widened(f.a[x / T]), c[x / T][x % T], 4, 4, BYTE, (int)s[T + x % T],
+                                                                          BYTE, (int)s[x / T]);
 }
 
 template <bool OUT_BF16, int T>
@@ -600,25 +608,47 @@ __global__ __launch_bounds__(256, 1) void matmul_tiles_kernel(const TilesArgs p)
         }
         arrived<0>();       // nothing is on its way into LDS that the next block may have
     }
-    const size_t base = (size_t)split * p.M * p.N;      // of partial sums; split is 0 where there are none
+    // The result leaves through LDS, 32 rows of a wave at a time, so that a store takes 1 KB and whole lines: from where the sums are it would be 16 or 8 bytes a lane of 32
+    // rows.  Each wave has a part of the ring to itself.
     typedef typename std::conditional<OUT_BF16, __bf16, float>::type Out;
-    Out *out = static_cast<Out *>(p.out) + base + (size_t)(m0 + ma) * p.ld + n0 + nb + r;
-    const bool whole = last_a + 1 >= B && last_b + 1 >= B;
+    typedef typename std::conditional<OUT_BF16, bf16x4, f32x4>::type Four;
+    typedef typename std::conditional<OUT_BF16, u32x4_bf16, u32x4_f32>::type Vector;
+    constexpr uint32_t kPer = 16 / sizeof(Out), kChunks = 32 * T / kPer, kRows = 64 / kChunks, kStrip = 32 * kChunks * 16;
+    const size_t base = (size_t)split * p.M * p.N;      // of partial sums; split is 0 where there are none
+    Out *out = static_cast<Out *>(p.out) + base + (size_t)(m0 + ma) * p.ld + n0 + nb;
+    char *mine = lds + wave * (kRing / 4);
+    __builtin_amdgcn_s_barrier();       // all have read what the ring held
+    const uint32_t of = lane / kChunks, chunk_out = lane % kChunks;
+    const bool inside = nb + (chunk_out + 1) * kPer <= last_b + 1;
 #pragma unroll
-    for (int i = 0; i < T; ++i)
+    for (int i = 0; i < T; ++i) {
+        char *strip = mine + (i & 1) * kStrip;
+        // chunk c of row r at place c ^ r, for the banks' sake
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const uint32_t row = i * 32 + 8 * (e / 4) + 4 * q + e % 4;
-            Out *to_row = out + row * p.ld;
-            if (whole) {
+        for (int k = 0; k < T; ++k)
 #pragma unroll
-                for (int k = 0; k < T; ++k) to_row[k * 32] = (Out)c[i][k][e];
-            } else if (ma + row <= last_a) {
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t col = k * 32 + 8 * e + 4 * q, at = (col / kPer) ^ (r & (kChunks - 1));
+                Four v;
 #pragma unroll
-                for (int k = 0; k < T; ++k)
-                    if (nb + k * 32 + r <= last_b) to_row[k * 32] = (Out)c[i][k][e];
+                for (int x = 0; x < 4; ++x) v[x] = (Out)c[i][k][4 * e + x];
+                *reinterpret_cast<Four *>(strip + (r * kChunks + at) * 16 + col % kPer * sizeof(Out)) = v;
             }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (uint32_t j = 0; j < 32 / kRows; ++j) {
+            const uint32_t row = j * kRows + of;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(strip + (row * kChunks + (chunk_out ^ (row & (kChunks - 1)))) * 16);
+            if (ma + i * 32 + row > last_a) continue;
+            Out *to = out + (size_t)(i * 32 + row) * p.ld + chunk_out * kPer;
+            if (inside && p.kept) store_through(to, v);
+            else if (inside) __builtin_nontemporal_store(v, reinterpret_cast<Vector *>(to));
+            else
+#pragma unroll
+                for (uint32_t x = 0; x < kPer; ++x)
+                    if (nb + chunk_out * kPer + x <= last_b) to[x] = __builtin_bit_cast(typename std::conditional<OUT_BF16, bf16x8, f32x4>::type, v)[x];
         }
+    }
 }
 
 struct JoinArgs {
@@ -636,11 +666,14 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
     const uint32_t n = size - at < 4 ? (uint32_t)(size - at) : 4u;
     f32x4 s = {0, 0, 0, 0};
     typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    // the loads of eight parts go out together
     if (n == 4) {
+#pragma unroll 8
         for (uint32_t k = 0; k < p.splits; ++k) s += *reinterpret_cast<const f32x4_any *>(p.parts + k * size + at);
     } else {
-        for (uint32_t k = 0; k < p.splits; ++k)
-            for (uint32_t i = 0; i < n; ++i) s[i] += p.parts[k * size + at + i];
+        for (uint32_t i = 0; i < n; ++i)
+#pragma unroll 8
+            for (uint32_t k = 0; k < p.splits; ++k) s[i] += p.parts[k * size + at + i];
     }
     uint32_t row = (uint32_t)(at / p.N), col = (uint32_t)(at - (size_t)row * p.N);
     for (uint32_t i = 0; i < n; ++i) {
@@ -656,12 +689,14 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
 // takes 256 bytes of a row and many are on the way.
 
 struct LinearArgs {
-    const void *x;
+    const void *x;             // or x's codes
+    const uint32_t *sx;        // their scales
     const uint8_t *w;
     const uint32_t *sw;
     void *out;
-    size_t ldx, ldo;
+    size_t ldx, ldt, ldn;      // of x; of the result from one of x's rows to the next, and from one of w's
     uint32_t T, N, K, groups;
+    uint32_t rows_x, rows_w;   // from one group's scales to the next one's
     uint32_t first;            // row of w that the launch begins with
     uint32_t log_split;
 };
@@ -754,6 +789,39 @@ __device__ __forceinline__ void bring_x(LinearShared<STEPS, DEPTH> &shared, cons
     }
 }
 
+// x is in MX4 already
+struct Codes {};
+
+template <int STEPS, int DEPTH>
+__device__ __forceinline__ void bring_codes(LinearShared<STEPS, DEPTH> &shared, const LinearArgs &a, uint32_t base, uint32_t steps) {
+    // 16 lanes a step of a row
+    constexpr uint32_t kAtOnce = 4, kThreads = 64 * kLinearWaves;
+    const uint32_t block = threadIdx.x & 15u, items = a.T * steps, part = 65536 / a.T + 1;
+    for (uint32_t first = threadIdx.x / 16; first < items; first += kAtOnce * (kThreads / 16)) {
+        u32x4 v[kAtOnce];
+        uint32_t s[kAtOnce];
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            const uint32_t wanted = first + k * (kThreads / 16), item = wanted < items ? wanted : items - 1;
+            const uint32_t step = item * part >> 16, token = item - step * a.T;       // divided by T: exact for the few items
+            const uint32_t group = (base + step) * kLinearGroups + block / 4, of_scale = (base + step) * kLinearGroups + (block & 3u);
+            const uint32_t last = a.groups - 1;
+            v[k] = *reinterpret_cast<const u32x4 *>(static_cast<const uint8_t *>(a.x) + (size_t)token * a.groups * kGroupBytes + (size_t)(group < last ? group : last) * kGroupBytes +
+                                                    (block & 3u) * 16);
+            s[k] = a.sx[(size_t)(of_scale < last ? of_scale : last) * a.rows_x + token];
+            if (group > last) v[k] = u32x4{0, 0, 0, 0};
+            if (of_scale > last) s[k] = 0;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            const uint32_t item = first + k * (kThreads / 16), step = item * part >> 16, token = item - step * a.T;
+            if (item >= items) break;
+            shared.codes[step][block][token ^ block] = v[k];
+            if (block < 4) shared.scales[step][block * 16 + token] = s[k];
+        }
+    }
+}
+
 template <typename T, bool OUT_BF16, bool ONCE, int STEPS, int DEPTH>
 __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearArgs a) {
     __shared__ LinearShared<STEPS, DEPTH> shared;
@@ -765,12 +833,12 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
     // Rows beyond w read as zero.  Groups beyond the last are the next row's codes, with scales that read as zero; x's codes are zero there.
     const uint32_t rows = n0 < a.N ? (a.N - n0 < 16 ? a.N - n0 : 16) : 0;
     const ss::Window ww = ss::window(a.w, (size_t)(rows ? n0 : 0) * row_bytes, rows * row_bytes);
-    const ss::Window ws = ss::window(a.sw, 0, a.groups * a.N * 4);
+    const ss::Window ws = ss::window(a.sw, 0, ((a.groups - 1) * a.rows_w + a.N) * 4);
     typedef __attribute__((address_space(3))) void *Lds;
     uint32_t from[4];       // 16 lanes take 256 bytes of a row, chunk c of row r to place c ^ r
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) from[i] = (4 * i + q) * row_bytes + ((r ^ (4 * i + q)) * 16);
-    const uint32_t from_s = (q * a.N + (n0 + r < a.N ? n0 + r : a.N - 1)) * 4;
+    const uint32_t from_s = (q * a.rows_w + (n0 + r < a.N ? n0 + r : a.N - 1)) * 4;
     // Rows that begin a power of two apart begin in the same memory channels: each wave begins at another of its steps
     const uint32_t per = STEPS >> a.log_split, tile = n0 / 16, tail = mine & (per - 1), turn = tile & (per - 1), turn_tail = tail ? uniform(tile % tail) : 0;
     auto step_of = [&](uint32_t k) {
@@ -785,7 +853,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ww, (Lds)(shared.w[wave][place] + i * 1024), 16, (int)from[i], (int)(step * (kLinearGroups * kGroupBytes)), 0, ONCE ? 2 : 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ws, (Lds)(shared.w[wave][place] + kLinearCodeBytes), 4, (int)from_s, (int)(step * kLinearGroups * a.N * 4), 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ws, (Lds)(shared.w[wave][place] + kLinearCodeBytes), 4, (int)from_s, (int)(step * kLinearGroups * a.rows_w * 4), 0, 0);
     };
     f32x4 c = {0, 0, 0, 0};
     uint32_t k = 0, place = 0;
@@ -797,7 +865,12 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
 #pragma unroll
             for (int i = 0; i < DEPTH; ++i) fetch((uint32_t)i, (uint32_t)i);
         };
-        bring_x<T>(shared, a, base, count, lane, wave, start);
+        if constexpr (std::is_same<T, Codes>::value) {
+            start();
+            bring_codes(shared, a, base, count);
+        } else {
+            bring_x<T>(shared, a, base, count, lane, wave, start);
+        }
         __syncthreads();
         const uint32_t end = mine < ((base + STEPS) >> a.log_split) ? mine : (base + STEPS) >> a.log_split;
         for (; k < end; ++k) {
@@ -831,7 +904,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t t = 4 * q + i;
-        if (t < a.T && n < a.N) store_out<OUT_BF16>(a.out, (size_t)t * a.ldo + n, c[i]);
+        if (t < a.T && n < a.N) store_out<OUT_BF16>(a.out, (size_t)t * a.ldt + n * a.ldn, c[i]);
     }
 }
 

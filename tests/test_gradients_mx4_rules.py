@@ -53,11 +53,11 @@ def check_gpu_tests_reach_both_sides(k):
     tiles, parts, splits = set(), set(), set()
     for M, N, K in gpu.PRODUCTS:
         got = k.of(k.matmul, M, N, K)
-        products = [s for s in got if "matmul_tiles" in s]
-        tiles.update(numbers(s)[1] for s in products)
+        products = [s for s in got if "join" not in s]
+        tiles.update(numbers(s)[1] if "matmul_tiles" in s else "few" for s in products)
         parts.add(len(products))
         splits.add(len(got) > len(products))
-    assert tiles == {1, 2, 4} and parts == {1, 2, 3} and splits == {False, True}, (tiles, parts, splits)
+    assert tiles == {1, 2, 4, "few"} and parts == {1, 2, 3} and splits == {False, True}, (tiles, parts, splits)
     shapes = {numbers(s)[1:] for N, K in gpu.LINEARS for s in k.of(k.linear, 1, N, K)}
     assert shapes == {(once, steps, depth) for once in (0, 1) for steps, depth in ((8, 3), (16, 2))}, shapes
     sharers = {round(8 * k.linear(1, N, K)[1][0][0] / -(-N // 16)) for N, K in gpu.LINEARS}       # waves to the same rows, of a block's eight
