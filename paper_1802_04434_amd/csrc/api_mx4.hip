@@ -25,7 +25,7 @@ inline bool bad_matrix(size_t rows, size_t cols, size_t ld) {
 }
 
 // From here on a matrix is read with nt: it is not in the memory-side cache.  us, without / with, 8192 x 8192: bf16 (134 MB) rows 30.5 / 28.0, columns 41.5 / 38.3,
-// both 47.8 / 43.6, fp32 52.1 / 47.6, 61.6 / 54.4, 68.6 / 62.4; 4096 x 8192 bf16 (67 MB), found there, 13.4 / 14.8, 20.4 / 21.8, 25.4 / 26.7.
+// both 47.8 / 43.6, fp32 52.1 / 47.6, 61.6 / 54.4, 68.6 / 62.4; 4096 x 8192 bf16 (67 MB), found there, 13.4 / 14.8, 20.4 / 21.8, 25.4 / 26.7 (before both took less).
 constexpr size_t kQuantizeOnce = (size_t)1 << 27;
 
 template <typename T>

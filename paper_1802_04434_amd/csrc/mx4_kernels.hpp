@@ -53,7 +53,6 @@ __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_floa
 __device__ __forceinline__ uint32_t dpp_xor1(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1 /* quad_perm [1,0,3,2] */, 0xF, 0xF, false); }
 __device__ __forceinline__ uint32_t dpp_xor2(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E /* quad_perm [2,3,0,1] */, 0xF, 0xF, false); }
 __device__ __forceinline__ uint32_t dpp_mirror8(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141 /* row_half_mirror */, 0xF, 0xF, false); }
-__device__ __forceinline__ uint32_t dpp_mirror16(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x140 /* row_mirror */, 0xF, 0xF, false); }
 
 // lane SEL of each four, for each of them; the lane N further on of 16
 template <int SEL>
@@ -115,12 +114,6 @@ struct F32 {
         o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[2][c]), __uint_as_float(v[3][c]), scale, 1);
         o = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[4][c]), __uint_as_float(v[5][c]), scale, 2);
         return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(o, __uint_as_float(v[6][c]), __uint_as_float(v[7][c]), scale, 3);
-    }
-    // the four scale bytes of 128 columns as a dword, in all of their 32 lanes
-    static __device__ __forceinline__ uint32_t gather_bytes(uint32_t byte, uint32_t lane) {
-        uint32_t v = byte << ((lane >> 3 & 3u) * 8);
-        v |= dpp_mirror16(v);
-        return v | (uint32_t)__shfl_xor((int)v, 16);
     }
 };
 
@@ -195,11 +188,6 @@ struct Bf16 {
         o = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, two(4), scale, 2);
         return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(o, two(6), scale, 3);
     }
-    static __device__ __forceinline__ uint32_t gather_bytes(uint32_t byte, uint32_t lane) {
-        uint32_t v = byte << ((lane >> 2 & 3u) * 8);
-        v |= dpp_mirror8(v);
-        return v | dpp_mirror16(v);
-    }
 };
 
 struct QuantizeArgs {
@@ -256,22 +244,33 @@ __device__ __forceinline__ void load_rows(u32x4 (&v)[R], const QuantizeArgs &a, 
     }
 }
 
+// Four rows' parts, of which a lane of four finds one's scale for all of them: their codes, and in lane k the dword of the scales of row k & 3 and of the lane's group
+template <typename T>
+__device__ __forceinline__ uint32_t quantize_four(const u32x4 (&v)[4], uint32_t lane, uint32_t (&codes)[4]) {
+    uint32_t bits[4];
+    T::four_max(v, bits);
+    const uint32_t byte = scale_byte(lane & 2u ? (lane & 1u ? bits[3] : bits[2]) : (lane & 1u ? bits[1] : bits[0])), scale = __float_as_uint(scale_of(byte));
+    codes[0] = T::row_codes(v[0], __uint_as_float(dpp_quad<0x00>(scale)));
+    codes[1] = T::row_codes(v[1], __uint_as_float(dpp_quad<0x55>(scale)));
+    codes[2] = T::row_codes(v[2], __uint_as_float(dpp_quad<0xAA>(scale)));
+    codes[3] = T::row_codes(v[3], __uint_as_float(dpp_quad<0xFF>(scale)));
+    return T::gather_four(byte, lane);
+}
+
 // Along the rows alone: a wave takes R rows of 64 lanes' columns, four waves a block one below the other.
 template <typename T, int R, bool ONCE, bool INSIDE>
 __device__ __forceinline__ void quantize_rows(const QuantizeArgs &a, uint32_t lane, uint32_t row0, uint32_t col) {
     const uint32_t padded = (a.cols + 127u) & ~127u;
     u32x4 v[R];
     load_rows<T, R, INSIDE, ONCE>(v, a, row0, col);
+    static_assert(R == 4, "");
+    uint32_t codes[4];
+    const uint32_t scales = quantize_four<T>(v, lane, codes);
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const uint32_t byte = scale_byte(T::row_max(T::magnitudes(v[r])));
-        const uint32_t codes = T::row_codes(v[r], scale_of(byte)), four = T::gather_bytes(byte, lane);
-        const uint32_t row = row0 + r;
-        if (INSIDE || (row < a.rows && col < padded)) {
-            T::store_row_codes(a.data + (size_t)row * (padded / 2) + col / 2, codes);
-            if ((lane & (4 * T::kLanes - 1)) == 0) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = four;
-        }
-    }
+    for (int r = 0; r < R; ++r)
+        if (INSIDE || (row0 + r < a.rows && col < padded)) T::store_row_codes(a.data + (size_t)(row0 + r) * (padded / 2) + col / 2, codes[r]);
+    const uint32_t row = row0 + (lane & 3u);
+    if ((lane & (4 * T::kLanes - 1)) < 4 && (INSIDE || (row < a.rows && col < padded))) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = scales;
 }
 
 template <typename T, int R, bool ONCE>
@@ -303,24 +302,29 @@ __device__ __forceinline__ void quantize_both(const QuantizeArgs &a, BothShared<
     u32x4 v[R];
     load_rows<T, R, INSIDE, ONCE>(v, a, row0, col);
     u32x4 m = T::magnitudes(v[0]);
-#pragma unroll
-    for (int r = 1; r < R; ++r) m = T::larger(m, T::magnitudes(v[r]));
-    shared.largest[wave][lane] = m;
     if constexpr (ROWS) {
         constexpr uint32_t kGroupLanes = 4 * T::kLanes;        // whose blocks share a dword: 32 or 16
         uint32_t kept = 0;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const uint32_t byte = scale_byte(T::row_max(T::magnitudes(v[r])));
-            const uint32_t codes = T::row_codes(v[r], scale_of(byte)), four = T::gather_bytes(byte, lane);
-            const uint32_t row = row0 + r;
-            if (INSIDE || (row < a.rows && col < padded)) T::store_row_codes(a.data + (size_t)row * (padded / 2) + col / 2, codes);
-            // lane r of the group keeps row r's, so that they leave side by side
-            if ((lane & (kGroupLanes - 1)) == (uint32_t)r) kept = four;
+        for (int r = 0; r < R; r += 4) {
+            const u32x4 part[4] = {v[r], v[r + 1], v[r + 2], v[r + 3]};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m = T::larger(m, T::magnitudes(part[i]));
+            uint32_t codes[4];
+            const uint32_t scales = quantize_four<T>(part, lane, codes);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (INSIDE || (row0 + r + i < a.rows && col < padded)) T::store_row_codes(a.data + (size_t)(row0 + r + i) * (padded / 2) + col / 2, codes[i]);
+            // lane k of the group keeps row k's, so that they leave side by side
+            if ((lane & (kGroupLanes - 4)) == (uint32_t)r) kept = scales;
         }
         const uint32_t row = row0 + (lane & (kGroupLanes - 1));
         if ((lane & (kGroupLanes - 1)) < R && (INSIDE || (row < a.rows && col < padded))) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = kept;
+    } else {
+#pragma unroll
+        for (int r = 1; r < R; ++r) m = T::larger(m, T::magnitudes(v[r]));
     }
+    shared.largest[wave][lane] = m;
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kShare; ++k) m = T::larger(m, shared.largest[(wave & ~(uint32_t)(kShare - 1)) + k][lane]);
@@ -342,7 +346,7 @@ __global__ __launch_bounds__(64 * kBothWaves, 4) void quantize_both_kernel(const
     constexpr uint32_t kColumns = 64 * T::kPer, kThreads = 64 * kBothWaves, kPiece = kBothRows / 2, kPlaces = kGroupBytes / kPiece;
     __shared__ BothShared<T> shared;
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
-    const uint32_t band = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - band * a.chunks, row0 = band * 128 + wave * kBothRows;
+    const uint32_t from_last = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - from_last * a.chunks, band = (a.rows + 127) / 128 - 1 - from_last, row0 = band * 128 + wave * kBothRows;
     const uint32_t first = chunk * kColumns, col = first + lane * T::kPer;
     if (first + kColumns <= a.cols && band * 128 + 128 <= a.rows) quantize_both<T, ROWS, ONCE, true>(a, shared, lane, wave, row0, col);
     else quantize_both<T, ROWS, ONCE, false>(a, shared, lane, wave, row0, col);
@@ -729,20 +733,16 @@ __device__ __forceinline__ void bring_x(LinearShared<STEPS, DEPTH> &shared, cons
         for (uint32_t i = 0; i < 4; ++i) v[i] = T::load(x + (col + i * kWidth < last ? col + i * kWidth : last));
     };
     auto put = [&](const u32x4 (&v)[4], Item at) {
-        uint32_t bits[4];
-        T::four_max(v, bits);
-        const uint32_t mine = lane & 2u ? (lane & 1u ? bits[3] : bits[2]) : (lane & 1u ? bits[1] : bits[0]), byte = scale_byte(mine);
-        const uint32_t scale = __float_as_uint(scale_of(byte));
-        const float scales[4] = {__uint_as_float(dpp_quad<0x00>(scale)), __uint_as_float(dpp_quad<0x55>(scale)), __uint_as_float(dpp_quad<0xAA>(scale)),
-                                 __uint_as_float(dpp_quad<0xFF>(scale))};
+        uint32_t codes[4];
+        const uint32_t dword = quantize_four<T>(v, lane, codes);
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {
             const uint32_t part = at.four * 4 + i, block = (i % kParts) * (kWidth / kBlockCols) + lane / T::kLanes;
             // rows are mixed, so that a row's blocks lie in different banks
             uint8_t *to = reinterpret_cast<uint8_t *>(&shared.codes[part / kParts][block][at.token ^ block]);
-            T::store_row_codes(to + (lane & (T::kLanes - 1)) * (T::kPer / 2), T::row_codes(v[i], scales[i]));
+            T::store_row_codes(to + (lane & (T::kLanes - 1)) * (T::kPer / 2), codes[i]);
         }
-        const uint32_t dword = T::gather_four(byte, lane), part = at.four * 4 + (lane & 3u), group = part % kParts * (kWidth / kGroupCols) + lane / (4 * T::kLanes);
+        const uint32_t part = at.four * 4 + (lane & 3u), group = part % kParts * (kWidth / kGroupCols) + lane / (4 * T::kLanes);
         if ((lane & (4 * T::kLanes - 1)) < 4) shared.scales[part / kParts][group * 16 + at.token] = dword;
     };
     const uint32_t more = uniform(kLinearWaves / fours), rest = kLinearWaves - more * fours;
