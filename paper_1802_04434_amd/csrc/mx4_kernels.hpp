@@ -138,12 +138,6 @@ struct Bf16 {
         for (int k = 0; k < 4; ++k) o[k] = pk_umax16(a[k], b[k]);
         return o;
     }
-    static __device__ __forceinline__ uint32_t row_max(u32x4 m) {
-        uint32_t v = pk_umax16(pk_umax16(m[0], m[1]), pk_umax16(m[2], m[3]));
-        v = pk_umax16(v, dpp_xor1(v));
-        v = pk_umax16(v, dpp_xor2(v));
-        return umax(v << 16, v & 0xFFFF0000u);
-    }
     static __device__ __forceinline__ uint32_t pick(u32x4 m, int c) { return c & 1 ? m[c >> 1] & 0xFFFF0000u : m[c >> 1] << 16; }
     static __device__ __forceinline__ void four_max(const u32x4 (&v)[4], uint32_t (&bits)[4]) {
         uint32_t m[4];
@@ -257,7 +251,8 @@ __device__ __forceinline__ uint32_t quantize_four(const u32x4 (&v)[4], uint32_t 
     return T::gather_four(byte, lane);
 }
 
-// Along the rows alone: a wave takes R rows of 64 lanes' columns, four waves a block one below the other.
+// Along the rows alone: a wave takes R rows of 64 lanes' columns, four waves a block one below the other; 2 or 8 rows a wave were 10 % slower.  Memory bounds it: 8192 x 8192
+// bf16 28 us (6.0 TB/s, a copy of as many bytes 25), fp32 48 (6.3 TB/s); 257 x 1000 3.4, a launch.
 template <typename T, int R, bool ONCE, bool INSIDE>
 __device__ __forceinline__ void quantize_rows(const QuantizeArgs &a, uint32_t lane, uint32_t row0, uint32_t col) {
     const uint32_t padded = (a.cols + 127u) & ~127u;
@@ -285,6 +280,8 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a
 // Down the columns, and along the rows too where wanted, in one pass.  A wave holds R rows of 64 lanes' columns in registers, so that R of a
 // column's block are one lane's; 32 / R waves share a block and exchange its largest magnitudes.  A block's waves take 128 rows, of which a column's codes are 64
 // bytes: they go through LDS, so that they leave as such (straight from the lanes they would be a few bytes here and there).
+// us, 8192 x 8192 along both: bf16 41.9 (4.9 TB/s), fp32 60.1 (5.6 TB/s), where each by itself would take 28 + 38 and 48 + 54; 4099 x 8192 bf16 24.9.  What bounds it is that a block loads, computes and
+// stores one after the other and two of them fit a compute unit: a third one, with 80 registers, spills (45.7).
 constexpr int kBothRows = 16, kBothWaves = 128 / kBothRows;
 
 template <typename T>
@@ -346,6 +343,7 @@ __global__ __launch_bounds__(64 * kBothWaves, 4) void quantize_both_kernel(const
     constexpr uint32_t kColumns = 64 * T::kPer, kThreads = 64 * kBothWaves, kPiece = kBothRows / 2, kPlaces = kGroupBytes / kPiece;
     __shared__ BothShared<T> shared;
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
+    // the band that may be short comes first: 4099 x 8192 in bf16, 528 blocks on 512 places, 28.9 -> 27.2 us
     const uint32_t from_last = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - from_last * a.chunks, band = (a.rows + 127) / 128 - 1 - from_last, row0 = band * 128 + wave * kBothRows;
     const uint32_t first = chunk * kColumns, col = first + lane * T::kPer;
     if (first + kColumns <= a.cols && band * 128 + 128 <= a.rows) quantize_both<T, ROWS, ONCE, true>(a, shared, lane, wave, row0, col);
@@ -451,6 +449,11 @@ __device__ __forceinline__ void store_out(void *out, size_t at, float v) {
 // straight into LDS, which has room for five operands' steps: both of the one that is read, both of the next one and the first of the one
 // after that.  So there is always something to load: the second operand of the next step right after the last one's place is free, when it has
 // the rest of the step to arrive, then the first one of the step after it, spread over the multiplications.
+//
+// The matrix unit bounds it, and that the card's power: multiplying registers of random codes without a load reaches 6.75 PFLOP/s.  8192 x 8192 x 16384 to fp32 466 to 480 us (4.7 PFLOP/s), of
+// which bringing the operands costs 50 and 67 MB of results at the end of each of four rounds 14 a round; 4096 cubed to bf16 34 to 36 us (3.9 PFLOP/s).  In 16 x 16 x
+// 128 it is no faster (532 us): a scaled multiplication takes two issue slots, and one wave a SIMD has no more of them.  Smaller tiles (T = 2, 1) are for results that do not
+// fill the card in large ones; which, the cost model on the host says.
 struct TilesArgs {
     const uint8_t *a, *b;
     const uint32_t *sa, *sb;
@@ -662,7 +665,7 @@ struct JoinArgs {
     uint32_t M, N, splits;
 };
 
-// the partial sums, one after the other: four columns a lane where rows are aligned to it, rows of a block by its number
+// the partial sums, one after the other, four neighbours a lane.  64 x 64 x 16384 in 64 parts takes 7.1 us with the product (14.0 with one part's load at a time).
 template <bool OUT_BF16>
 __global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
     const size_t size = (size_t)p.M * p.N, at = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -690,7 +693,8 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs p) {
 // Up to 16 rows of x, quantised on the way.  A wave streams 16 rows of w, or SPLIT of a block's waves share them, each with every SPLIT-th step of 512
 // columns, and their sums are added through LDS in order.  A block first brings x in MX4 into LDS, or as many steps of it as fit, while its waves' first steps of w are on
 // the way.  What has to be read is w, and that is what bounds it: its steps go straight into LDS, each wave's into a ring of its own, so that a load
-// takes 256 bytes of a row and many are on the way.
+// takes 256 bytes of a row and many are on the way.  us, 8192 columns and 28672 rows of w (129 MB): one row of x 21.2 (5.9 TB/s), sixteen 27.0 (4.6 TB/s), where each block's
+// quantisation of x, about 60 MB of it out of the L2s, is 5; 4096 x 4096, one row 4.0 (a launch is 3.4), sixteen 7.
 
 struct LinearArgs {
     const void *x;             // or x's codes
@@ -839,7 +843,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
 #pragma unroll
     for (uint32_t i = 0; i < 4; ++i) from[i] = (4 * i + q) * row_bytes + ((r ^ (4 * i + q)) * 16);
     const uint32_t from_s = (q * a.rows_w + (n0 + r < a.N ? n0 + r : a.N - 1)) * 4;
-    // Rows that begin a power of two apart begin in the same memory channels: each wave begins at another of its steps
+    // Rows that begin a power of two apart begin in the same memory channels: each wave begins at another of its steps (8192 columns and 28672 rows 28.5 -> 23.1 us)
     const uint32_t per = STEPS >> a.log_split, tile = n0 / 16, tail = mine & (per - 1), turn = tile & (per - 1), turn_tail = tail ? uniform(tile % tail) : 0;
     auto step_of = [&](uint32_t k) {
         k = k < mine ? k : mine - 1;
