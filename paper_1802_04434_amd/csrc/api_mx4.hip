@@ -172,16 +172,17 @@ int ss_mx4_quantize(const void *x, ss_dtype xdt, size_t rows, size_t cols, size_
     if (written_spans_overlap(spans, 5)) return SS_ERR_ARG;
     mx4::QuantizeArgs a{x, data, reinterpret_cast<uint32_t *>(scales), data_t, reinterpret_cast<uint32_t *>(scales_t), ld,
                         (uint32_t)rows, (uint32_t)cols, 0};
-    const size_t per = 64 * (xdt == SS_BF16 ? mx4::Bf16::kPer : mx4::F32::kPer);
+    // columns of a block
+    const size_t per = xdt == SS_BF16 ? (data_t ? mx4::kAcross<mx4::Bf16> : 64) * mx4::Bf16::kPer : (data_t ? mx4::kAcross<mx4::F32> : 64) * mx4::F32::kPer;
     a.chunks = (uint32_t)((ss_mx4_padded(cols) + per - 1) / per);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     const bool once = rows * cols * grad_bytes(xdt) >= kQuantizeOnce;
     if (data_t) {
-        constexpr int kThreads = 64 * mx4::kBothWaves;
+        const int threads = xdt == SS_BF16 ? mx4::kBothThreads<mx4::Bf16> : mx4::kBothThreads<mx4::F32>;
         const size_t grid = a.chunks * groups_of(rows);
-        if (grid > kMaxThreads / kThreads) return SS_ERR_ARG;
+        if (grid > kMaxThreads / threads) return SS_ERR_ARG;
         const auto kernel = xdt == SS_BF16 ? both_kernel<mx4::Bf16>(data != nullptr, once) : both_kernel<mx4::F32>(data != nullptr, once);
-        return launch(kernel, grid, 0, stream, a, kThreads);
+        return launch(kernel, grid, 0, stream, a, threads);
     }
     constexpr int kRows = 4;
     const size_t grid = a.chunks * ((rows + 4 * kRows - 1) / (4 * kRows));

@@ -277,23 +277,28 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a
     else quantize_rows<T, R, ONCE, false>(a, lane, row0, col);
 }
 
-// Down the columns, and along the rows too where wanted, in one pass.  A wave holds R rows of 64 lanes' columns in registers, so that R of a
-// column's block are one lane's; 32 / R waves share a block and exchange its largest magnitudes.  A block's waves take 128 rows, of which a column's codes are 64
-// bytes: they go through LDS, so that they leave as such (straight from the lanes they would be a few bytes here and there).
-// us, 8192 x 8192 along both: bf16 41.9 (4.9 TB/s), fp32 60.1 (5.6 TB/s), where each by itself would take 28 + 38 and 48 + 54; 4099 x 8192 bf16 24.9.  What bounds it is that a block loads, computes and
-// stores one after the other and two of them fit a compute unit: a third one, with 80 registers, spills (45.7).
-constexpr int kBothRows = 16, kBothWaves = 128 / kBothRows;
+// Down the columns, and along the rows too where wanted, in one pass.  A lane holds 16 rows of 16 bytes in registers, so that half of a column's block is its own; the other half is
+// that of another lane, with which it compares its largest magnitudes.  A block takes 128 rows, of which a column's codes are 64 bytes: they go through LDS, so that they leave as
+// such (straight from the lanes they would be a few bytes here and there).  kAcross lanes take a row side by side: 32 of bf16, four blocks of which fit a compute unit, where a block of twice
+// the width, of which two do, takes 41.7 us for 37.3 at 8192 x 8192; but 64 of fp32, whose rows' codes are half as long (60.3 for 65.2).
+// us, 8192 x 8192 along both: bf16 37.3 (5.5 TB/s), fp32 60.3 (5.6 TB/s), where each by itself would take 28 + 35 and 48 + 54; 4099 x 8192 bf16 22.9.  What bounds it is that a block loads,
+// computes and stores one after the other: more of them do not fit the registers (80 of them: spills, 45.7).
+constexpr int kBothRows = 16;
+template <typename T>
+constexpr uint32_t kAcross = T::kPer == 8 ? 32 : 64;
+template <typename T>
+constexpr uint32_t kBothThreads = kAcross<T> * 128 / kBothRows;
 
 template <typename T>
 struct BothShared {
-    uint8_t codes[64 * T::kPer * kGroupBytes];
-    u32x4 largest[kBothWaves][64];
-    uint32_t scales[64 * T::kPer];
+    uint8_t codes[kAcross<T> * T::kPer * kGroupBytes];
+    u32x4 largest[kAcross<T> == 64 ? kBothThreads<T> : 1];
+    uint32_t scales[kAcross<T> * T::kPer];
 };
 
 template <typename T, bool ROWS, bool ONCE, bool INSIDE>
-__device__ __forceinline__ void quantize_both(const QuantizeArgs &a, BothShared<T> &shared, uint32_t lane, uint32_t wave, uint32_t row0, uint32_t col) {
-    constexpr int R = kBothRows, kShare = 32 / R;
+__device__ __forceinline__ void quantize_both(const QuantizeArgs &a, BothShared<T> &shared, uint32_t lane, uint32_t share, uint32_t row0, uint32_t col) {
+    constexpr int R = kBothRows;
     constexpr uint32_t kPiece = R / 2, kPlaces = kGroupBytes / kPiece;
     const uint32_t padded = (a.cols + 127u) & ~127u;
     u32x4 v[R];
@@ -321,33 +326,39 @@ __device__ __forceinline__ void quantize_both(const QuantizeArgs &a, BothShared<
 #pragma unroll
         for (int r = 1; r < R; ++r) m = T::larger(m, T::magnitudes(v[r]));
     }
-    shared.largest[wave][lane] = m;
-    __syncthreads();
+    u32x4 others;
+    if constexpr (kAcross<T> == 64) {
+        shared.largest[threadIdx.x] = m;
+        __syncthreads();
+        others = shared.largest[threadIdx.x ^ 64u];
+    } else {
 #pragma unroll
-    for (int k = 0; k < kShare; ++k) m = T::larger(m, shared.largest[(wave & ~(uint32_t)(kShare - 1)) + k][lane]);
+        for (int k = 0; k < 4; ++k) others[k] = (uint32_t)__shfl_xor((int)m[k], 32);
+    }
+    m = T::larger(m, others);
 #pragma unroll
     for (int c = 0; c < (int)T::kPer; ++c) {
         const uint32_t byte = scale_byte(T::pick(m, c));
         const float scale = scale_of(byte);
-        const uint32_t column = lane * T::kPer + c;
-        // piece w of a column at place w ^ lane, for the banks' sake
-        uint32_t *to = reinterpret_cast<uint32_t *>(shared.codes + column * kGroupBytes + ((wave ^ (lane & (kPlaces - 1))) * kPiece));
+        const uint32_t column = (lane & (kAcross<T> - 1)) * T::kPer + c;
+        // piece s of a column at place s ^ lane, for the banks' sake
+        uint32_t *to = reinterpret_cast<uint32_t *>(shared.codes + column * kGroupBytes + ((share ^ (lane & (kPlaces - 1))) * kPiece));
 #pragma unroll
         for (int k = 0; k < R / 8; ++k) to[k] = T::column_codes(v + 8 * k, c, scale);
-        if (wave % kShare == 0) reinterpret_cast<uint8_t *>(&shared.scales[column])[wave / kShare] = (uint8_t)byte;
+        if (share % 2 == 0) reinterpret_cast<uint8_t *>(&shared.scales[column])[share / 2] = (uint8_t)byte;
     }
 }
 
 template <typename T, bool ROWS, bool ONCE>
-__global__ __launch_bounds__(64 * kBothWaves, 4) void quantize_both_kernel(const QuantizeArgs a) {
-    constexpr uint32_t kColumns = 64 * T::kPer, kThreads = 64 * kBothWaves, kPiece = kBothRows / 2, kPlaces = kGroupBytes / kPiece;
+__global__ __launch_bounds__(kBothThreads<T>, 4) void quantize_both_kernel(const QuantizeArgs a) {
+    constexpr uint32_t kColumns = kAcross<T> * T::kPer, kThreads = kBothThreads<T>, kPiece = kBothRows / 2, kPlaces = kGroupBytes / kPiece;
     __shared__ BothShared<T> shared;
-    const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
-    // the band that may be short comes first: 4099 x 8192 in bf16, 528 blocks on 512 places, 28.9 -> 27.2 us
-    const uint32_t from_last = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - from_last * a.chunks, band = (a.rows + 127) / 128 - 1 - from_last, row0 = band * 128 + wave * kBothRows;
-    const uint32_t first = chunk * kColumns, col = first + lane * T::kPer;
-    if (first + kColumns <= a.cols && band * 128 + 128 <= a.rows) quantize_both<T, ROWS, ONCE, true>(a, shared, lane, wave, row0, col);
-    else quantize_both<T, ROWS, ONCE, false>(a, shared, lane, wave, row0, col);
+    const uint32_t lane = threadIdx.x & 63u, share = kAcross<T> == 64 ? uniform(threadIdx.x / 64) : threadIdx.x / 32;      // of the rows
+    // the band that may be short comes first: 4099 x 8192 in bf16, when its 528 blocks were to share 512 places, 28.9 -> 27.2 us
+    const uint32_t from_last = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - from_last * a.chunks, band = (a.rows + 127) / 128 - 1 - from_last, row0 = band * 128 + share * kBothRows;
+    const uint32_t first = chunk * kColumns, col = first + (lane & (kAcross<T> - 1)) * T::kPer;
+    if (first + kColumns <= a.cols && band * 128 + 128 <= a.rows) quantize_both<T, ROWS, ONCE, true>(a, shared, lane, share, row0, col);
+    else quantize_both<T, ROWS, ONCE, false>(a, shared, lane, share, row0, col);
     __syncthreads();
     const size_t row_bytes = (((size_t)a.rows + 127) & ~(size_t)127) / 2;
 #pragma unroll
@@ -566,10 +577,10 @@ __global__ __launch_bounds__(256, 1) void matmul_tiles_kernel(const TilesArgs p)
 #pragma unroll
         for (int i = 0; i < L; ++i) fetch_a(i, a, column_of(from)), fetch_b(i, b, column_of(from));
         fetch_scales(s, from);
-        arrived<0>();
-        __builtin_amdgcn_s_barrier();
 #pragma unroll
         for (int i = 0; i < L; ++i) fetch_a(i, a1, column_of(from + 1)), fetch_b(i, b1, column_of(from + 1));
+        arrived<2 * L>();
+        __builtin_amdgcn_s_barrier();
 #pragma unroll
         for (int i = 0; i < 2 * T; ++i) read(f0, i, 0, a, b);
         __builtin_amdgcn_sched_barrier(0);
