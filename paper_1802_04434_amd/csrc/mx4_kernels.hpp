@@ -461,8 +461,8 @@ __device__ __forceinline__ void store_out(void *out, size_t at, float v) {
 // after that.  So there is always something to load: the second operand of the next step right after the last one's place is free, when it has
 // the rest of the step to arrive, then the first one of the step after it, spread over the multiplications.
 //
-// The matrix unit bounds it, and that the card's power: multiplying registers of random codes without a load reaches 6.75 PFLOP/s.  8192 x 8192 x 16384 to fp32 466 to 480 us (4.7 PFLOP/s), of
-// which bringing the operands costs 50 and 67 MB of results at the end of each of four rounds 14 a round; 4096 cubed to bf16 34 to 36 us (3.9 PFLOP/s).  In 16 x 16 x
+// The matrix unit bounds it, and that the card's power: multiplying registers of random codes without a load reaches 6.75 PFLOP/s.  8192 x 8192 x 16384 to fp32 458 to 480 us (4.7 PFLOP/s), of
+// which bringing the operands costs 50 and 67 MB of results at the end of each of four rounds 14 a round; 4096 cubed to bf16 33 to 36 us (4.0 PFLOP/s).  In 16 x 16 x
 // 128 it is no faster (532 us): a scaled multiplication takes two issue slots, and one wave a SIMD has no more of them.  Smaller tiles (T = 2, 1) are for results that do not
 // fill the card in large ones; which, the cost model on the host says.
 struct TilesArgs {
