@@ -36,13 +36,13 @@ auto both_kernel(bool rows, bool once) {
 
 // Weights of 64 MB and more are read with nt, which leaves the caches to others: 21.4 instead of 23.1 us at 28672 by 8192.  Smaller ones may still be there from the
 // token before: 10.4 instead of 11.3 us at 16384 by 4096.
-constexpr size_t kLinearBlocks = 192, kLinearOnce = (size_t)1 << 26;
+constexpr size_t kLinearBlocks = 256, kLinearOnce = (size_t)1 << 26;
 
-// x in LDS: 4,096 columns at a time with three steps of w on the way for each wave, or 8,192 with two
+// x in LDS: 4,096 columns at a time with three steps of w on the way for each wave, or 10,240 with two, as many as there is room for
 template <typename T, bool OUT_BF16>
 auto linear_kernel(size_t steps, bool once) {
     if (steps <= 8) return once ? mx4::linear_kernel<T, OUT_BF16, true, 8, 3> : mx4::linear_kernel<T, OUT_BF16, false, 8, 3>;
-    return once ? mx4::linear_kernel<T, OUT_BF16, true, 16, 2> : mx4::linear_kernel<T, OUT_BF16, false, 16, 2>;
+    return once ? mx4::linear_kernel<T, OUT_BF16, true, 20, 2> : mx4::linear_kernel<T, OUT_BF16, false, 20, 2>;
 }
 
 template <typename T>
@@ -50,8 +50,9 @@ auto linear_kernel(ss_dtype odt, size_t steps, bool once) { return odt == SS_BF1
 
 inline int few_rows(decltype(linear_kernel<mx4::F32>) *kernels, ss_dtype odt, mx4::LinearArgs a, hipStream_t stream) {
     const size_t tiles = ((size_t)a.N + 15) / 16, steps = ((size_t)a.groups + mx4::kLinearGroups - 1) / mx4::kLinearGroups;
-    // as few waves to the same rows as fill the card: each block brings x
-    while (2u << a.log_split <= mx4::kLinearWaves && (tiles << a.log_split) < kLinearBlocks * mx4::kLinearWaves && (size_t)1 << a.log_split < steps) ++a.log_split;
+    // as many waves to the same rows as a block on each compute unit gives (one is all that LDS has room for).  us, 1 and 16 rows, 4096 to 5000 columns, in 157 blocks / 313: 4.6 and 7.5 /
+    // 7.0 and 12.4
+    while (2u << a.log_split <= mx4::kLinearWaves && (tiles << a.log_split) * 2 <= kLinearBlocks * mx4::kLinearWaves && (size_t)1 << a.log_split < steps) ++a.log_split;
     const auto kernel = kernels(odt, steps, (size_t)a.N * a.groups * mx4::kGroupBytes >= kLinearOnce);
     constexpr int kThreads = 64 * mx4::kLinearWaves;
     const size_t rows = 16 * (mx4::kLinearWaves >> a.log_split), most = kMaxThreads / kThreads;
@@ -98,10 +99,10 @@ inline Plan plan_of(size_t M, size_t N, size_t K, bool may_split) {
             if (us < best.us) best = Plan{s.tile, splits, us};
         }
     }
-    // The few rows' kernel: w's bytes, and what it costs to bring each 8,192 columns of x; tiles have to read w too.  us, few rows / tiles: 1 x 4096 x 4096 4.0 / 8.2, 16 x 8192 x
+    // The few rows' kernel: w's bytes, and what it costs to bring each 10,240 columns of x; tiles have to read w too.  us, few rows / tiles: 1 x 4096 x 4096 4.0 / 8.2, 16 x 8192 x
     // 4096 6.2 / 9.6, 16 x 16384 x 16384 28.2 / 31.7, but 16 x 16 x 32768, of which tiles can split the sum, 12.0 / 7.9
     if (std::min(M, N) <= SS_MX4_LINEAR_MAX_ROWS) {
-        const double bytes = (double)std::max(M, N) * groups_of(K) * 68, us = 2.0 + bytes / 6.5e6 + 2.6 * (double)((groups_of(K) - 1) / 64);
+        const double bytes = (double)std::max(M, N) * groups_of(K) * 68, us = 2.0 + bytes / 6.5e6 + 2.6 * (double)((groups_of(K) - 1) / 80);
         if (us < std::max(best.us, 3.0 + bytes / 4.6e6)) best = Plan{0, 1, us};
     }
     return best;

@@ -855,16 +855,19 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
     for (uint32_t i = 0; i < 4; ++i) from[i] = (4 * i + q) * row_bytes + ((r ^ (4 * i + q)) * 16);
     const uint32_t from_s = (q * a.rows_w + (n0 + r < a.N ? n0 + r : a.N - 1)) * 4;
     // Rows that begin a power of two apart begin in the same memory channels: each wave begins at another of its steps (8192 columns and 28672 rows 28.5 -> 23.1 us)
-    const uint32_t per = STEPS >> a.log_split, tile = n0 / 16, tail = mine & (per - 1), turn = tile & (per - 1), turn_tail = tail ? uniform(tile % tail) : 0;
-    auto step_of = [&](uint32_t k) {
-        k = k < mine ? k : mine - 1;
-        const uint32_t base = k & ~(per - 1), left = mine - base < per ? tail : per;
-        uint32_t i = k - base + (mine - base < per ? turn_tail : turn);
+    const uint32_t per = STEPS >> a.log_split, pass = per << a.log_split, tile = n0 / 16;       // of a pass' steps so many are this wave's
+    const uint32_t tail = uniform(mine % per), turn = uniform(tile % per), turn_tail = tail ? uniform(tile % tail) : 0;
+    // step k of this wave, which is in the pass that begins with `begin`, or after it
+    auto step_of = [&](uint32_t k, uint32_t begin) {
+        if (k >= mine) k = mine - 1;
+        while (k >= begin + per) begin += per;
+        const uint32_t left = mine - begin < per ? tail : per;
+        uint32_t i = k - begin + (mine - begin < per ? turn_tail : turn);
         if (i >= left) i -= left;
-        return ((base + i) << a.log_split) + share;
+        return ((begin + i) << a.log_split) + share;
     };
-    auto fetch = [&](uint32_t place, uint32_t k) {
-        const uint32_t step = mine ? step_of(k) : 0;
+    auto fetch = [&](uint32_t place, uint32_t k, uint32_t begin) {
+        const uint32_t step = mine ? step_of(k, begin) : 0;
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ww, (Lds)(shared.w[wave][place] + i * 1024), 16, (int)from[i], (int)(step * (kLinearGroups * kGroupBytes)), 0, ONCE ? 2 : 0);
@@ -872,13 +875,13 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
     };
     f32x4 c = {0, 0, 0, 0};
     uint32_t k = 0, place = 0;
-    for (uint32_t base = 0; base < steps; base += STEPS) {
-        const uint32_t count = steps - base < STEPS ? steps - base : STEPS;
+    for (uint32_t base = 0; base < steps; base += pass) {
+        const uint32_t count = steps - base < pass ? steps - base : pass, begin = k;
         if (base) __syncthreads();
         auto start = [&] {
             if (base) return;
 #pragma unroll
-            for (int i = 0; i < DEPTH; ++i) fetch((uint32_t)i, (uint32_t)i);
+            for (int i = 0; i < DEPTH; ++i) fetch((uint32_t)i, (uint32_t)i, 0);
         };
         if constexpr (std::is_same<T, Codes>::value) {
             start();
@@ -887,24 +890,24 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
             bring_x<T>(shared, a, base, count, lane, wave, start);
         }
         __syncthreads();
-        const uint32_t end = mine < ((base + STEPS) >> a.log_split) ? mine : (base + STEPS) >> a.log_split;
+        const uint32_t end = mine < begin + per ? mine : begin + per;
         for (; k < end; ++k) {
-                arrived<5 * (DEPTH - 1)>();
-                u32x4 f[4], g[4];
-                const uint32_t at = step_of(k) - base;
+            arrived<5 * (DEPTH - 1)>();
+            u32x4 f[4], g[4];
+            const uint32_t at = step_of(k, begin) - base;
 #pragma unroll
-                for (uint32_t j = 0; j < 4; ++j) {
-                    g[j] = *reinterpret_cast<const u32x4 *>(shared.w[wave][place] + r * 256 + (((q * 4 + j) ^ r) * 16));
-                    f[j] = shared.codes[at][q * 4 + j][r ^ (q * 4 + j)];
-                }
-                const uint32_t sx = shared.scales[at][lane], sn = reinterpret_cast<const uint32_t *>(shared.w[wave][place] + kLinearCodeBytes)[lane];
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                fetch(place, k + DEPTH);
-                place = place + 1 < DEPTH ? place + 1 : 0;
-                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[0]), widened(g[0]), c, 4, 4, 0, (int)sx, 0, (int)sn);
-                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[1]), widened(g[1]), c, 4, 4, 1, (int)sx, 1, (int)sn);
-                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[2]), widened(g[2]), c, 4, 4, 2, (int)sx, 2, (int)sn);
-                c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[3]), widened(g[3]), c, 4, 4, 3, (int)sx, 3, (int)sn);
+            for (uint32_t j = 0; j < 4; ++j) {
+                g[j] = *reinterpret_cast<const u32x4 *>(shared.w[wave][place] + r * 256 + (((q * 4 + j) ^ r) * 16));
+                f[j] = shared.codes[at][q * 4 + j][r ^ (q * 4 + j)];
+            }
+            const uint32_t sx = shared.scales[at][lane], sn = reinterpret_cast<const uint32_t *>(shared.w[wave][place] + kLinearCodeBytes)[lane];
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            fetch(place, k + DEPTH, begin);
+            place = place + 1 < DEPTH ? place + 1 : 0;
+            c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[0]), widened(g[0]), c, 4, 4, 0, (int)sx, 0, (int)sn);
+            c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[1]), widened(g[1]), c, 4, 4, 1, (int)sx, 1, (int)sn);
+            c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[2]), widened(g[2]), c, 4, 4, 2, (int)sx, 2, (int)sn);
+            c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(widened(f[3]), widened(g[3]), c, 4, 4, 3, (int)sx, 3, (int)sn);
         }
     }
     arrived<0>();       // nothing is on its way into LDS that others may have

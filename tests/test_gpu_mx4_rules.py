@@ -12,7 +12,7 @@ PRODUCTS = [(1, 64, 20_000), (40, 4096, 4096), (64, 16_384, 100), (255, 256, 819
             (1024, 1024, 16_000), (1153, 2177, 640), (2048, 2048, 300), (2049, 2049, 2048), (2050, 4100, 1000), (4096, 4096, 129), (4099, 8192, 256), (4097, 4098, 700), (2052, 4099, 16_000), (2084, 4130, 8192),
             (1, 1, 8192), (16, 17, 600), (17, 16, 600), (5, 700, 70), (700, 5, 4097), (7, 16_384, 8192), (32_768, 3, 4096), (16, 2000, 9000), (15, 33, 70_000)]
 LINEARS = [(700, 4096), (6000, 3000), (9000, 4097), (12_288, 1000), (12_289, 4096), (16_384, 8192), (16_383, 8192), (24_576, 700), (32_768, 4096), (32_767, 4096),
-           (40_000, 9000), (4097, 32_800)]
+           (40_000, 9000), (4097, 32_800), (300, 10_240), (300, 10_241), (20_000, 10_000), (5000, 4096), (33_000, 600)]
 MATRICES = [(8192, 8191), (8192, 8192), (4096, 8192), (4096, 8191), (8320, 8300)]
 
 

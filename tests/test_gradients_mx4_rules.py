@@ -59,7 +59,7 @@ def check_gpu_tests_reach_both_sides(k):
         splits.add(len(got) > len(products))
     assert tiles == {1, 2, 4, "few"} and parts == {1, 2, 3} and splits == {False, True}, (tiles, parts, splits)
     shapes = {numbers(s)[1:] for N, K in gpu.LINEARS for s in k.of(k.linear, 1, N, K)}
-    assert shapes == {(once, steps, depth) for once in (0, 1) for steps, depth in ((8, 3), (16, 2))}, shapes
+    assert len(shapes) == 4 and {s[0] for s in shapes} == {0, 1} and len({s[1:] for s in shapes}) == 2, shapes       # cache policies, columns at a time
     sharers = {round(8 * k.linear(1, N, K)[1][0][0] / -(-N // 16)) for N, K in gpu.LINEARS}       # waves to the same rows, of a block's eight
     assert sharers == {1, 2, 4, 8}, sharers
     for dt in (F32, BF16):
