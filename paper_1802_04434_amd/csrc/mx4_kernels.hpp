@@ -723,6 +723,18 @@ struct LinearArgs {
 constexpr int kLinearWaves = 8;
 constexpr uint32_t kLinearGroups = 4, kLinearCodeBytes = 16 * kLinearGroups * kGroupBytes, kLinearStepBytes = kLinearCodeBytes + 16 * kLinearGroups * 4;     // a step of 16 rows: codes, scales
 
+// The scales of one step, for the first n of a matrix' rows: where they begin, in bytes, and how many of them can be read.  A large matrix has more than 4 GiB of scales, which 32 bits do not
+// address; of a step there are 2 GiB at most.
+struct ScaleWindow {
+    size_t from;
+    uint32_t bytes;
+};
+
+constexpr ScaleWindow scale_window(uint32_t groups, uint32_t step, uint32_t rows, uint32_t n) {
+    const uint32_t first = step * kLinearGroups, left = groups - first;
+    return {(size_t)first * rows * 4, (((left < kLinearGroups ? left : kLinearGroups) - 1) * rows + n) * 4};
+}
+
 // STEPS of x in LDS, DEPTH of w for each wave
 template <int STEPS, int DEPTH>
 struct LinearShared {
@@ -848,7 +860,6 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
     // Rows beyond w read as zero.  Groups beyond the last are the next row's codes, with scales that read as zero; x's codes are zero there.
     const uint32_t rows = n0 < a.N ? (a.N - n0 < 16 ? a.N - n0 : 16) : 0;
     const ss::Window ww = ss::window(a.w, (size_t)(rows ? n0 : 0) * row_bytes, rows * row_bytes);
-    const ss::Window ws = ss::window(a.sw, 0, ((a.groups - 1) * a.rows_w + a.N) * 4);
     typedef __attribute__((address_space(3))) void *Lds;
     uint32_t from[4];       // 16 lanes take 256 bytes of a row, chunk c of row r to place c ^ r
 #pragma unroll
@@ -868,10 +879,12 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
     };
     auto fetch = [&](uint32_t place, uint32_t k, uint32_t begin) {
         const uint32_t step = mine ? step_of(k, begin) : 0;
+        const ScaleWindow s = scale_window(a.groups, step, a.rows_w, a.N);
+        const ss::Window ws = ss::window(a.sw, s.from, s.bytes);
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ww, (Lds)(shared.w[wave][place] + i * 1024), 16, (int)from[i], (int)(step * (kLinearGroups * kGroupBytes)), 0, ONCE ? 2 : 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ws, (Lds)(shared.w[wave][place] + kLinearCodeBytes), 4, (int)from_s, (int)(step * kLinearGroups * a.rows_w * 4), 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ws, (Lds)(shared.w[wave][place] + kLinearCodeBytes), 4, (int)from_s, 0, 0, 0);
     };
     f32x4 c = {0, 0, 0, 0};
     uint32_t k = 0, place = 0;
