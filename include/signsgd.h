@@ -443,7 +443,7 @@ int ss_mx4_matmul(const uint8_t *a_data, const uint8_t *a_scales, const uint8_t 
 /*
  * out (T x N) <- x w^T for the few rows of an answering model: x of T x K (T at most
  * SS_MX4_LINEAR_MAX_ROWS, else SS_ERR_ARG) is quantised on the way as ss_mx4_quantize does it,
- * w of N x K is in MX4.  No memory for x in MX4 is needed; one launch (per 134 million rows of w).
+ * w of N x K is in MX4.  No memory for x in MX4 is needed; one launch.
  */
 #define SS_MX4_LINEAR_MAX_ROWS 16
 int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8_t *w_data,

@@ -55,13 +55,9 @@ inline int few_rows(decltype(linear_kernel<mx4::F32>) *kernels, ss_dtype odt, mx
     while (2u << a.log_split <= mx4::kLinearWaves && (tiles << a.log_split) * 2 <= kLinearBlocks * mx4::kLinearWaves && (size_t)1 << a.log_split < steps) ++a.log_split;
     const auto kernel = kernels(odt, steps, (size_t)a.N * a.groups * mx4::kGroupBytes >= kLinearOnce);
     constexpr int kThreads = 64 * mx4::kLinearWaves;
-    const size_t rows = 16 * (mx4::kLinearWaves >> a.log_split), most = kMaxThreads / kThreads;
-    for (size_t first = 0; first < a.N; first += most * rows) {
-        a.first = (uint32_t)first;
-        const int rc = launch(kernel, std::min((a.N - first + rows - 1) / rows, most), 0, stream, a, kThreads);
-        if (rc != SS_OK) return rc;
-    }
-    return SS_OK;
+    static_assert(SS_MX4_MAX_DIM / 16 / mx4::kLinearWaves * kThreads <= kMaxThreads, "one launch takes all rows");      // 16 a wave where there are many
+    const size_t rows = 16 * (mx4::kLinearWaves >> a.log_split);
+    return launch(kernel, ((size_t)a.N + rows - 1) / rows, 0, stream, a, kThreads);
 }
 
 // How a product, or a part of one, is cut: tiles of 64 times `tile` squared (0: a few rows or columns of the result, by the kernel for them), and the sum over the
@@ -248,7 +244,7 @@ int ss_mx4_matmul(const uint8_t *a_data, const uint8_t *a_scales, const uint8_t 
             const uint32_t rows[2] = {(uint32_t)M, (uint32_t)N};
             const int rc = few_rows(linear_kernel<mx4::Codes>, odt,
                                     {data[!wide], scales[!wide], data[wide], scales[wide], to, 0, wide ? ld : 1, wide ? 1 : ld, (uint32_t)std::min(part.M, part.N),
-                                     (uint32_t)std::max(part.M, part.N), (uint32_t)K, (uint32_t)groups, rows[!wide], rows[wide], 0, 0},
+                                     (uint32_t)std::max(part.M, part.N), (uint32_t)K, (uint32_t)groups, rows[!wide], rows[wide], 0},
                                     stream);
             if (rc != SS_OK) return rc;
             continue;
@@ -284,7 +280,7 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
     if (written_spans_overlap(spans, 4)) return SS_ERR_ARG;
     return few_rows(xdt == SS_BF16 ? linear_kernel<mx4::Bf16> : linear_kernel<mx4::F32>, odt,
                     {x, nullptr, w_data, reinterpret_cast<const uint32_t *>(w_scales), out, ldx, ldo, 1, (uint32_t)T, (uint32_t)N, (uint32_t)K, (uint32_t)groups_of(K), 0,
-                     (uint32_t)N, 0, 0},
+                     (uint32_t)N, 0},
                     static_cast<hipStream_t>(hip_stream));
 }
 

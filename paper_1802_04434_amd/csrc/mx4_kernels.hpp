@@ -716,7 +716,6 @@ struct LinearArgs {
     size_t ldx, ldt, ldn;      // of x; of the result from one of x's rows to the next, and from one of w's
     uint32_t T, N, K, groups;
     uint32_t rows_x, rows_w;   // from one group's scales to the next one's
-    uint32_t first;            // row of w that the launch begins with
     uint32_t log_split;
 };
 
@@ -854,7 +853,7 @@ __global__ __launch_bounds__(64 * kLinearWaves) void linear_kernel(const LinearA
     __shared__ LinearShared<STEPS, DEPTH> shared;
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6), r = lane & 15u, q = lane >> 4;
     const uint32_t split = 1u << a.log_split, share = wave & (split - 1);
-    const uint32_t n0 = a.first + (blockIdx.x * (kLinearWaves >> a.log_split) + (wave >> a.log_split)) * 16;
+    const uint32_t n0 = (blockIdx.x * (kLinearWaves >> a.log_split) + (wave >> a.log_split)) * 16;
     const uint32_t steps = (a.groups + kLinearGroups - 1) / kLinearGroups, mine = steps > share ? (steps - share + split - 1) >> a.log_split : 0;
     const uint32_t row_bytes = a.groups * kGroupBytes;
     // Rows beyond w read as zero.  Groups beyond the last are the next row's codes, with scales that read as zero; x's codes are zero there.
