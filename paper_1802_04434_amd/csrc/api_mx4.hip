@@ -181,11 +181,11 @@ int ss_mx4_quantize(const void *x, ss_dtype xdt, size_t rows, size_t cols, size_
         const auto kernel = xdt == SS_BF16 ? both_kernel<mx4::Bf16>(data != nullptr, once) : both_kernel<mx4::F32>(data != nullptr, once);
         return launch(kernel, grid, 0, stream, a, threads);
     }
-    constexpr int kRows = 4;
-    const size_t grid = a.chunks * ((rows + 4 * kRows - 1) / (4 * kRows));
+    constexpr size_t kRows = 4 * mx4::kQuantizeRows;       // of a block
+    const size_t grid = a.chunks * ((rows + kRows - 1) / kRows);
     if (grid > kMaxThreads / 256) return SS_ERR_ARG;
-    const auto kernel = xdt == SS_BF16 ? (once ? mx4::quantize_rows_kernel<mx4::Bf16, kRows, true> : mx4::quantize_rows_kernel<mx4::Bf16, kRows, false>)
-                                       : (once ? mx4::quantize_rows_kernel<mx4::F32, kRows, true> : mx4::quantize_rows_kernel<mx4::F32, kRows, false>);
+    const auto kernel = xdt == SS_BF16 ? (once ? mx4::quantize_rows_kernel<mx4::Bf16, true> : mx4::quantize_rows_kernel<mx4::Bf16, false>)
+                                       : (once ? mx4::quantize_rows_kernel<mx4::F32, true> : mx4::quantize_rows_kernel<mx4::F32, false>);
     return launch(kernel, grid, 0, stream, a, 256);
 }
 

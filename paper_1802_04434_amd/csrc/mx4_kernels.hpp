@@ -212,8 +212,8 @@ __device__ __forceinline__ u32x4 load_part(const QuantizeArgs &a, uint32_t row, 
     return v;
 }
 
-// R rows' parts, out together; INSIDE: nothing ends in them.  The rows are the same for all lanes, so that their addresses are the scalar unit's.  Where the
-// matrix ends a lane loads what ends with it and drops the front, so that no load waits for a test: waited for one by one 16 rows took 8 us.
+// R rows' parts, out together; INSIDE: nothing ends in them.  But for bf16 down the columns, where half a wave has other rows, they are the same for all lanes, so that their addresses are the
+// scalar unit's.  Where the matrix ends a lane loads what ends with it and drops the front, so that no load waits for a test: waited for one by one 16 rows took 8 us.
 template <typename T, int R, bool INSIDE, bool ONCE>
 __device__ __forceinline__ void load_rows(u32x4 (&v)[R], const QuantizeArgs &a, uint32_t row0, uint32_t col) {
     const typename T::elem *x = static_cast<const typename T::elem *>(a.x);
@@ -251,30 +251,30 @@ __device__ __forceinline__ uint32_t quantize_four(const u32x4 (&v)[4], uint32_t 
     return T::gather_four(byte, lane);
 }
 
-// Along the rows alone: a wave takes R rows of 64 lanes' columns, four waves a block one below the other; 2 or 8 rows a wave were 10 % slower.  Memory bounds it: 8192 x 8192
+// Along the rows alone: a wave takes four rows of 64 lanes' columns, four waves a block one below the other; 2 or 8 rows a wave were 10 % slower.  Memory bounds it: 8192 x 8192
 // bf16 28 us (6.0 TB/s, a copy of as many bytes 25), fp32 48 (6.3 TB/s); 257 x 1000 3.4, a launch.
-template <typename T, int R, bool ONCE, bool INSIDE>
+constexpr int kQuantizeRows = 4;
+template <typename T, bool ONCE, bool INSIDE>
 __device__ __forceinline__ void quantize_rows(const QuantizeArgs &a, uint32_t lane, uint32_t row0, uint32_t col) {
     const uint32_t padded = (a.cols + 127u) & ~127u;
-    u32x4 v[R];
-    load_rows<T, R, INSIDE, ONCE>(v, a, row0, col);
-    static_assert(R == 4, "");
-    uint32_t codes[4];
+    u32x4 v[kQuantizeRows];
+    load_rows<T, kQuantizeRows, INSIDE, ONCE>(v, a, row0, col);
+    uint32_t codes[kQuantizeRows];
     const uint32_t scales = quantize_four<T>(v, lane, codes);
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int r = 0; r < kQuantizeRows; ++r)
         if (INSIDE || (row0 + r < a.rows && col < padded)) T::store_row_codes(a.data + (size_t)(row0 + r) * (padded / 2) + col / 2, codes[r]);
     const uint32_t row = row0 + (lane & 3u);
     if ((lane & (4 * T::kLanes - 1)) < 4 && (INSIDE || (row < a.rows && col < padded))) a.scales[(size_t)(col / kGroupCols) * a.rows + row] = scales;
 }
 
-template <typename T, int R, bool ONCE>
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const QuantizeArgs a) {
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
-    const uint32_t band = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - band * a.chunks, row0 = (band * 4 + wave) * R;
+    const uint32_t band = uniform(blockIdx.x / a.chunks), chunk = blockIdx.x - band * a.chunks, row0 = (band * 4 + wave) * kQuantizeRows;
     const uint32_t col = (chunk * 64 + lane) * T::kPer;
-    if ((chunk + 1) * 64 * T::kPer <= a.cols && row0 + R <= a.rows) quantize_rows<T, R, ONCE, true>(a, lane, row0, col);
-    else quantize_rows<T, R, ONCE, false>(a, lane, row0, col);
+    if ((chunk + 1) * 64 * T::kPer <= a.cols && row0 + kQuantizeRows <= a.rows) quantize_rows<T, ONCE, true>(a, lane, row0, col);
+    else quantize_rows<T, ONCE, false>(a, lane, row0, col);
 }
 
 // Down the columns, and along the rows too where wanted, in one pass.  A lane holds 16 rows of 16 bytes in registers, so that half of a column's block is its own; the other half is
