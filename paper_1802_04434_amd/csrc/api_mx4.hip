@@ -24,8 +24,8 @@ inline bool bad_matrix(size_t rows, size_t cols, size_t ld) {
     return rows > SS_MX4_MAX_DIM || cols > SS_MX4_MAX_DIM || ld < cols || ld > ((size_t)1 << 40) || rows * cols > SS_MX4_MAX_ELEMENTS;
 }
 
-// From here on a matrix is read with nt: it is not in the memory-side cache.  us, without / with, 8192 x 8192: bf16 (134 MB) rows 30.5 / 28.0, columns 41.5 / 38.3,
-// both 47.8 / 43.6, fp32 52.1 / 47.6, 61.6 / 54.4, 68.6 / 62.4; 4096 x 8192 bf16 (67 MB), found there, 13.4 / 14.8, 20.4 / 21.8, 25.4 / 26.7 (before both took less).
+// From here on a matrix is read with nt: it is not in the memory-side cache.  us along the rows, the columns and both, without / with, three matrices in turn: 8192 x 8192 fp32 (268 MB) 51.8 /
+// 48.0, 59.7 / 54.8, 65.4 / 60.5; in bf16 (134 MB), where it makes little difference, 28.2 / 28.8, 34.5 / 35.5, 37.8 / 37.8; 4096 x 8192 bf16 (67 MB), found there, 13.2 / 14.8, 14.9 / 17.3, 17.7 / 21.5.
 constexpr size_t kQuantizeOnce = (size_t)1 << 27;
 
 template <typename T>

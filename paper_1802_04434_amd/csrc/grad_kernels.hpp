@@ -71,9 +71,9 @@ __device__ __forceinline__ bool edge_element(uint32_t lane, uint32_t lead, size_
 // Block b takes units [U b / G, U (b + 1) / G) of U, BATCH of them in flight; the lanes' sums in fp64 go through lane moves and LDS
 // into a slot, and the block that takes the last ticket adds the slots in a fixed order and writes the norm.  As in the density few large
 // blocks, since tickets on one address take 11 ns each; here they are taken in two levels, 16 groups on lines of their own and one
-// above, 32 in a row instead of 256.  Of several launches all but the last one add to the slots and take no tickets.
-// Measured: 1.5 G bf16 436 us (6.9 TB/s), 25.6 M fp32 in 161 tensors 21 (4.9 TB/s), of which launch, ramp and the tail of dependent trips are 6; 272,474 in 65 tensors 5.3, of which the
-// host's call alone is 5.2.
+// above: 48 in a row instead of 512, and 32 instead of 256 from a GiB on.  Of several launches all but the last one add to the slots and take no tickets.
+// Measured, us: 1.5 G bf16 436 to 457 (6.6 to 6.9 TB/s), 25.6 M fp32 in 161 tensors 20 (5.2 TB/s), of which ramp and the tail of dependent trips are 5; 272,474 in 65
+// tensors 5.4, of which the host's call alone is 5.2.
 
 constexpr int kNormThreads = 512;
 constexpr int kNormBlocks = 512;
@@ -233,7 +233,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(const NormArgs a) {
 // ---------------------------------------------------------------- clip ----
 // A block takes kClipRows rows of 16 bytes a lane, aligned to 16 bytes where they are written; they are read at whatever address that gives.  Many short blocks, since there is nothing
 // to add up: us for 25.6 M fp32 in 161 tensors, 1 / 2 / 8 rows 48 / 31 / 42, and runs of units a block 40 to 48.  That is 6.5 TB/s, what a copy takes;
-// 138 M of both types into fp32 165 us (5.6 TB/s).
+// 138 M of both types into fp32 160 us (5.6 TB/s).  The other forms on 25.6 M: fp32 to bf16 26 us (5.9 TB/s), bf16 to bf16 17.5 (5.8), bf16 to fp32
+// 26 (5.9), in place fp32 36 (5.7) and bf16 18 (5.7), and within the bound, where nothing is to do, 5.0 and 3.5.
 
 constexpr int kClipThreads = 256;
 template <bool IN_BF16, bool OUT_BF16>

@@ -386,7 +386,8 @@ struct DequantizeArgs {
     uint32_t chunks;           // of 512 columns
 };
 
-// A lane takes eight codes, a wave R rows of 512 columns.  Stored with nt: 8192 x 8192 bf16 25.0 us (6.8 TB/s) against 33.4.
+// A lane takes eight codes, a wave R rows of 512 columns.  Stored with nt: 8192 x 8192 bf16 25.0 us (6.8 TB/s) against 33.4.  To fp32, a lane's 32 bytes in two stores, 116 us (2.6
+// TB/s).
 template <bool OUT_BF16, int R>
 __global__ __launch_bounds__(256) void dequantize_kernel(const DequantizeArgs a) {
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
@@ -461,8 +462,8 @@ __device__ __forceinline__ void store_out(void *out, size_t at, float v) {
 // after that.  So there is always something to load: the second operand of the next step right after the last one's place is free, when it has
 // the rest of the step to arrive, then the first one of the step after it, spread over the multiplications.
 //
-// The matrix unit bounds it, and that the card's power: multiplying registers of random codes without a load reaches 6.75 PFLOP/s.  8192 x 8192 x 16384 to fp32 458 to 480 us (4.7 PFLOP/s), of
-// which bringing the operands costs 50 and 67 MB of results at the end of each of four rounds 14 a round; 4096 cubed to bf16 33 to 36 us (4.0 PFLOP/s).  In 16 x 16 x
+// The matrix unit bounds it, and that the card's power: multiplying registers of random codes without a load reaches 6.75 PFLOP/s.  8192 x 8192 x 16384 to fp32 458 to 490 us (4.5 to 4.8 PFLOP/s), by card and day, of
+// which bringing the operands costs 50, and in each of four rounds nothing is multiplied for 3 at the start and for 14 at the end, while 67 MB of results leave; 4096 cubed to bf16 32 to 36 us (4.0 PFLOP/s).  In 16 x 16 x
 // 128 it is no faster (532 us): a scaled multiplication takes two issue slots, and one wave a SIMD has no more of them.  Smaller tiles (T = 2, 1) are for results that do not
 // fill the card in large ones; which, the cost model on the host says.
 struct TilesArgs {
