@@ -450,6 +450,91 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
                   const uint8_t *w_scales, size_t N, size_t K, void *out, ss_dtype odt,
                   size_t ldo, void *hip_stream);
 
+/* ---- the loss over a vocabulary, and its gradient ----
+ *
+ * Softmax cross entropy of T rows h (T x K) against a head w (V x K), z = h w^T, without keeping z: the
+ * last layer of a language model, whose logits would be its largest matrix.  h and w are bf16 (dt:
+ * SS_BF16, else SS_ERR_DTYPE), products are exact, sums in fp32.
+ *   h, w     in   a row every ldh / ldw elements, aligned to their element alone
+ *   target   in   T int64 in DEVICE memory.  Below 0: the row has none; it adds nothing to any gradient,
+ *                 whatever its entries of h are (infinities and NaN included).  V or more: the row's
+ *                 loss, and with it the gradients, are NaN.
+ *   scratch  work ss_cross_entropy_scratch_bytes(T, V, K) bytes of DEVICE memory, 16-byte aligned,
+ *                 contents immaterial before and after; untouched by others until the enqueued work
+ *                 has run (two calls that may run at the same time, or two captured graphs that may,
+ *                 need two).  Smaller: SS_ERR_ARG.
+ * T may be 0; V and K may not, and none may exceed the limits below (SS_ERR_ARG).  Nothing that is written
+ * may share a byte with anything else of the call.  Rows whose K is a multiple of 64, whose ld is one of 8 and
+ * that are 16-byte aligned are read where they are; others are copied into scratch on the way, piece by piece.
+ * Sums are added in an order that depends on the sizes and on that alone.
+ */
+#define SS_LOSS_MAX_ROWS ((size_t)1 << 24)
+#define SS_LOSS_MAX_VOCAB ((size_t)1 << 24)
+#define SS_LOSS_MAX_WIDTH ((size_t)1 << 20)
+size_t ss_cross_entropy_scratch_bytes(size_t T, size_t V, size_t K);
+
+/*
+ * lse_t <- log sum_v exp(z_tv);  loss_t <- lse_t - z_t,target_t, 0 in rows without a target.
+ *   loss, lse  out  T x fp32.  A row with an infinite or NaN logit has NaN, but one of -infinity
+ *                   next to finite ones counts as zero probability.
+ */
+int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V,
+                     size_t K, size_t ldw, const int64_t *target, float *loss, float *lse,
+                     void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/*
+ * With D_tv = dloss_t (exp(z_tv - lse_t) - [v = target_t]), 0 in rows without a target:
+ * dh <- D w, dw <- D^T h, sums in fp32, rounded once to the gradient's type.  D is rounded to
+ * bf16 on the way, relative to the largest |dloss| (2^-9 of an entry at most).
+ *   lse      in   T x fp32, as ss_cross_entropy leaves it
+ *   dloss    in   T x fp32: the weight of each row (1 / their number for a mean), NULL: 1
+ *   dh, dw   out  T x K and V x K, bf16 or fp32, a row every lddh / lddw elements, aligned to
+ *                 their element; either may be NULL: not wanted.
+ */
+int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V,
+                          size_t K, size_t ldw, const int64_t *target, const float *lse,
+                          const float *dloss, void *dh, ss_dtype dhdt, size_t lddh, void *dw,
+                          ss_dtype dwdt, size_t lddw, void *scratch, size_t scratch_bytes,
+                          void *hip_stream);
+
+/* ---- a matrix's step: the update orthogonalised ----
+ *
+ * Where a vector's step takes the sign of every entry of the momentum (steepest descent in the max
+ * norm), a matrix's takes that of every singular value (steepest descent in the spectral norm), by
+ * Newton-Schulz products:
+ *     X = g / |g|_F;  `steps` times  A = X X^T,  X <- 3.4445 X - 4.7750 A X + 2.0315 A A X
+ * (transposed where g has more rows than columns; five steps bring every singular value above 0.01 of the
+ * norm to between 0.68 and 1.2).  A matrix of zeros gives zeros; one with an infinity or a NaN, NaN everywhere.
+ * The scale of g makes no difference.  Products take operands of 11 bits, X is held in 22 and sums in fp32: five steps are off by
+ * 1e-3 to 2e-3 of the result's norm, which is what rounding it to bf16 costs.
+ *   count, rows, cols   a stack of matrices, each by itself; any may be 0
+ *   ld, apart           elements from one row to the next, and from one matrix to the next
+ *   scratch             ss_orthogonalize_scratch_bytes(count, rows, cols) bytes, under the same terms
+ *                       as that of ss_cross_entropy
+ */
+#define SS_ORTHOGONAL_MAX_COUNT ((size_t)65535)
+#define SS_ORTHOGONAL_MAX_DIM ((size_t)1 << 20)
+#define SS_ORTHOGONAL_MAX_SHORT ((size_t)1 << 15)      /* the shorter side */
+#define SS_ORTHOGONAL_MAX_ELEMENTS ((size_t)1 << 33)   /* of the stack */
+#define SS_ORTHOGONAL_MAX_STEPS 100
+size_t ss_orthogonalize_scratch_bytes(size_t count, size_t rows, size_t cols);
+
+/* out <- g orthogonalised; both fp32 or bf16, aligned to their element alone.  Nothing may overlap, from
+ * a buffer's first to its last element. */
+int ss_orthogonalize(const void *g, ss_dtype gdt, size_t count, size_t rows, size_t cols, size_t ld,
+                     size_t apart, int steps, void *out, ss_dtype odt, size_t ldo, size_t aparto,
+                     void *scratch, size_t scratch_bytes, void *hip_stream);
+
+/*
+ * The whole step of a matrix:  m <- beta m + (1 - beta) g (rounded as in ss_signum_pack);
+ * u = m, or with `ahead` (0 or 1) beta m + (1 - beta) g;  x <- x - delta (u orthogonalised).
+ *   m, x   i/o  count x rows x cols fp32 without gaps, aligned to their element (parts of a parameter vector)
+ */
+int ss_orthogonal_step(const void *g, ss_dtype gdt, size_t count, size_t rows, size_t cols,
+                       size_t ld, size_t apart, float *m, float beta, int ahead, int steps,
+                       float delta, float *x, void *scratch, size_t scratch_bytes,
+                       void *hip_stream);
+
 /* the hipError_t (as int) behind this thread's most recent SS_ERR_HIP; 0 if none */
 int ss_last_hip_error(void);
 

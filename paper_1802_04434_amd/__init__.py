@@ -15,4 +15,6 @@ from .binding import (  # noqa: F401
     quorum_vote, signum_pack_ternary, signum_vote_step_ternary, ternary_apply,
     grad_clip, grad_norm, new_grad_norm_workspace,
     Mx4, mx4_dequantize, mx4_linear, mx4_matmul, mx4_quantize, new_mx4,
+    cross_entropy, cross_entropy_grad, new_cross_entropy_scratch,
+    new_orthogonalize_scratch, orthogonal_step, orthogonalize,
 )

@@ -94,8 +94,16 @@ def load_library():
         L.ss_mx4_matmul_scratch_bytes.argtypes = [sz, sz, sz]
         L.ss_mx4_matmul.argtypes = [vp, vp, vp, vp, sz, sz, sz, vp, i32, sz, vp, sz, vp]
         L.ss_mx4_linear.argtypes = [vp, i32, sz, sz, vp, vp, sz, sz, vp, i32, sz, vp]
+        L.ss_cross_entropy_scratch_bytes.restype = sz
+        L.ss_cross_entropy_scratch_bytes.argtypes = [sz, sz, sz]
+        L.ss_cross_entropy.argtypes = [vp, i32, sz, sz, vp, sz, sz, sz, vp, vp, vp, vp, sz, vp]
+        L.ss_cross_entropy_grad.argtypes = [vp, i32, sz, sz, vp, sz, sz, sz, vp, vp, vp, vp, i32, sz, vp, i32, sz, vp, sz, vp]
+        L.ss_orthogonalize_scratch_bytes.restype = sz
+        L.ss_orthogonalize_scratch_bytes.argtypes = [sz, sz, sz]
+        L.ss_orthogonalize.argtypes = [vp, i32, sz, sz, sz, sz, sz, i32, vp, i32, sz, sz, vp, sz, vp]
+        L.ss_orthogonal_step.argtypes = [vp, i32, sz, sz, sz, sz, sz, vp, f32, i32, i32, f32, vp, vp, sz, vp]
         for name in ("ss_grad_norm", "ss_grad_clip", "ss_mx4_quantize", "ss_mx4_dequantize", "ss_mx4_matmul",
-                     "ss_mx4_linear"):
+                     "ss_mx4_linear", "ss_cross_entropy", "ss_cross_entropy_grad", "ss_orthogonalize", "ss_orthogonal_step"):
             getattr(L, name).restype = i32
         for name in ("ss_signum_pack_ternary", "ss_quorum_vote", "ss_ternary_apply",
                      "ss_signum_vote_step_ternary"):
@@ -340,3 +348,48 @@ def mx4_linear(x, w, out, stream=None):
     """ss_mx4_linear: out <- x w^T for up to 16 rows of x (float32 or bfloat16), which is quantised on the way"""
     _check("ss_mx4_linear", (_marshal or _native()).mx4_linear(x, w, out, stream))
     return out
+
+
+# ---- the loss over a vocabulary ----
+
+def new_cross_entropy_scratch(rows, vocab, width, device="cuda"):
+    """work memory for cross_entropy and cross_entropy_grad of rows x width against vocab x width, kept by the caller; two
+    calls that may overlap in time need two"""
+    return torch.empty(load_library().ss_cross_entropy_scratch_bytes(rows, vocab, width), dtype=torch.uint8, device=device)
+
+
+def cross_entropy(h, w, target, loss, lse, scratch, stream=None):
+    """ss_cross_entropy: lse[t] <- log sum_v exp(z[t, v]), loss[t] <- lse[t] - z[t, target[t]] with z = h w^T, which is not kept.
+    h: T x K and w: V x K, bfloat16, elements of a row side by side; target: T int64, below 0 where a row has none (loss 0);
+    loss, lse: T float32; scratch: new_cross_entropy_scratch(T, V, K)."""
+    _check("ss_cross_entropy", (_marshal or _native()).cross_entropy(h, w, target, loss, lse, scratch, stream))
+    return loss
+
+
+def cross_entropy_grad(h, w, target, lse, dloss, dh, dw, scratch, stream=None):
+    """ss_cross_entropy_grad: the gradients of sum_t dloss[t] loss[t] by h and by w, rows without a target left out whatever they hold.
+    lse: as cross_entropy left it; dloss: T float32, or None for ones; dh, dw: bfloat16 or float32, of h's and w's shape, either
+    may be None."""
+    _check("ss_cross_entropy_grad", (_marshal or _native()).cross_entropy_grad(h, w, target, lse, dloss, dh, dw, scratch, stream))
+
+
+# ---- a matrix's step ----
+
+def new_orthogonalize_scratch(rows, cols, count=1, device="cuda"):
+    """work memory for orthogonalize and orthogonal_step of `count` matrices, kept by the caller; two calls that may overlap in
+    time need two"""
+    return torch.empty(load_library().ss_orthogonalize_scratch_bytes(count, rows, cols), dtype=torch.uint8, device=device)
+
+
+def orthogonalize(g, out, scratch, steps=5, stream=None):
+    """ss_orthogonalize: out <- g with every singular value brought near 1 by `steps` Newton-Schulz steps.
+    g, out: rows x cols or count x rows x cols, float32 or bfloat16, elements of a row side by side."""
+    _check("ss_orthogonalize", (_marshal or _native()).orthogonalize(g, out, scratch, steps, stream))
+    return out
+
+
+def orthogonal_step(g, m, beta, delta, x, scratch, ahead=False, steps=5, stream=None):
+    """ss_orthogonal_step: m <- beta m + (1 - beta) g; x <- x - delta * orthogonalize(m, or with `ahead` beta m + (1 - beta) g).
+    g as above; m, x: contiguous float32 of its shape (views of a parameter vector's parts)."""
+    _check("ss_orthogonal_step", (_marshal or _native()).orthogonal_step(g, m, beta, delta, x, scratch, ahead, steps, stream))
+    return x

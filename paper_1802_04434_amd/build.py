@@ -12,7 +12,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsignsgd.so")
-SOURCES = ["api.hip", "api_grad.hip", "api_mx4.hip"]
+SOURCES = ["api.hip", "api_grad.hip", "api_mx4.hip", "api_loss.hip", "api_orthogonal.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,0 +1,220 @@
+// C ABI of the loss over a vocabulary and its gradient (see include/signsgd.h): validation, pieces and launches.
+#include <algorithm>
+
+#include "api_common.hpp"
+#include "loss_kernels.hpp"
+#include "product_launch.hpp"
+
+namespace {
+
+using namespace host;
+using product::Layout;
+using product::Operand;
+using product::Plan;
+using product::Product;
+using product::rounded;
+using product::tiles_of;
+
+inline bool element_aligned(const void *p, ss_dtype dt) { return reinterpret_cast<uintptr_t>(p) % grad_bytes(dt) == 0; }
+
+inline Span matrix(const void *p, size_t rows, size_t cols, size_t ld, ss_dtype dt, bool written) {
+    return span(p, rows && cols ? ((rows - 1) * ld + cols) * grad_bytes(dt) : 0, written);
+}
+
+inline bool bad_sizes(size_t T, size_t V, size_t K) { return T > SS_LOSS_MAX_ROWS || V > SS_LOSS_MAX_VOCAB || K == 0 || K > SS_LOSS_MAX_WIDTH || V == 0; }
+inline bool bad_ld(size_t ld, size_t cols) { return ld < cols || ld > 2 * SS_LOSS_MAX_WIDTH; }
+
+// whether the products can load a matrix as it lies: whole steps of k, rows at multiples of 16 bytes
+inline bool loadable(const void *p, size_t K, size_t ld) { return K % product::kStep == 0 && ld % 8 == 0 && aligned16(p); }
+
+// What is computed at a time is a piece of the vocabulary.  Forward: 2^36 entries of z, or 128 MB of copied weights.  Backward: 128 MB of D, so that
+// the products that read it find it in the memory-side cache.
+constexpr size_t kPieceEntries = (size_t)1 << 26, kForwardEntries = (size_t)1 << 36, kEdge = 256;
+
+inline size_t piece_of(size_t entries, size_t rows, size_t V) { return std::min(std::max(entries / rows / kEdge * kEdge, 4 * kEdge), rounded(V, kEdge)); }
+
+struct Sizes {
+    size_t T, V, K, T64, K64;
+    Sizes(size_t t, size_t v, size_t k) : T(t), V(v), K(k), T64(rounded(t, 64)), K64(rounded(k, 64)) {}
+    size_t copied() const { return piece_of(kPieceEntries, K64, V); }       // rows of weights in a copy
+    size_t forward(bool copy) const { return std::min(piece_of(kForwardEntries, T64, V), copy ? copied() : V); }
+    size_t backward(bool copy) const { return std::min(piece_of(kPieceEntries, T64, V), copy ? copied() : V); }
+};
+
+struct ForwardPlace {
+    size_t parts, picked, h, w, bytes;
+    ForwardPlace(const Sizes &s) {
+        Layout l;
+        size_t most = 0;
+        for (const bool copy : {false, true}) {
+            size_t count = 0;
+            for (size_t v = 0; v < s.V; v += s.forward(copy)) {
+                const size_t n = std::min(s.forward(copy), s.V - v);
+                count += 2 * tiles_of(n, product::plan_of(s.T, n, s.K64, 1, false).tile);
+            }
+            most = std::max(most, count);
+        }
+        parts = l.take(most * s.T * sizeof(loss::Part));
+        picked = l.take(s.T * sizeof(float));
+        h = l.take(s.T64 * s.K64 * 2);
+        w = l.take(s.copied() * s.K64 * 2);
+        bytes = l.bytes;
+    }
+};
+
+struct BackwardPlace {
+    size_t factor, scale, h, d, w, sum, parts, bytes;
+    BackwardPlace(const Sizes &s) {
+        Layout l;
+        const size_t most = rounded(s.backward(false), 64);
+        factor = l.take(s.T64 * sizeof(float));
+        scale = l.take(sizeof(float));
+        h = l.take(s.T64 * s.K64 * 2);
+        d = l.take(s.T64 * most * 2);
+        w = l.take(s.copied() * s.K64 * 2);
+        sum = l.take(s.T * s.K * sizeof(float));
+        size_t of_parts = 0;
+        for (const bool copy : {false, true}) {
+            const size_t piece = std::min(s.backward(copy), s.V), last = s.V - (s.V - 1) / piece * piece;
+            for (const size_t n : {piece, last}) {
+                of_parts = std::max(of_parts, parts_bytes(product::plan_of(s.T, s.K, rounded(n, 64), 1, true), 1, s.T, s.K));
+                of_parts = std::max(of_parts, parts_bytes(product::plan_of(n, s.K, s.T64, 1, true), 1, n, s.K));
+            }
+        }
+        parts = l.take(of_parts);
+        bytes = l.bytes;
+    }
+};
+
+int copied(const void *from, size_t ld_from, void *to, size_t rows, size_t cols, size_t ld, size_t lines, const int64_t *target, hipStream_t stream) {
+    const loss::CopyArgs a{static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to), target, ld_from, (uint32_t)rows, (uint32_t)cols, (uint32_t)ld, (uint32_t)lines,
+                           ld_from % 8 == 0 && aligned16(from)};
+    return launch(loss::copy_kernel, (lines * (ld / 8) + 255) / 256, 0, stream, a, 256);
+}
+
+int check(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V, size_t K, size_t ldw, const int64_t *target) {
+    if (dt != SS_BF16) return SS_ERR_DTYPE;
+    if (bad_sizes(T, V, K) || bad_ld(ldh, K) || bad_ld(ldw, K)) return SS_ERR_ARG;
+    if (T == 0) return SS_OK;
+    if (!h || !w || !target) return SS_ERR_NULL;
+    if (!element_aligned(h, dt) || !element_aligned(w, dt) || reinterpret_cast<uintptr_t>(target) % 8) return SS_ERR_ALIGN;
+    return SS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ss_cross_entropy_scratch_bytes(size_t T, size_t V, size_t K) {
+    if (bad_sizes(T, V, K) || T == 0) return 0;
+    const Sizes s(T, V, K);
+    return std::max(ForwardPlace(s).bytes, BackwardPlace(s).bytes);
+}
+
+int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V, size_t K, size_t ldw, const int64_t *target,
+                     float *loss, float *lse, void *scratch, size_t scratch_bytes, void *hip_stream) {
+    int rc = check(h, dt, T, ldh, w, V, K, ldw, target);
+    if (rc != SS_OK || T == 0) return rc;
+    if (!loss || !lse || !scratch) return SS_ERR_NULL;
+    if (!element_aligned(loss, SS_F32) || !element_aligned(lse, SS_F32) || !aligned16(scratch)) return SS_ERR_ALIGN;
+    Span spans[6] = {matrix(h, T, K, ldh, dt, false), matrix(w, V, K, ldw, dt, false), span(target, T * 8, false), span(loss, T * 4, true), span(lse, T * 4, true),
+                     span(scratch, scratch_bytes, true)};
+    if (written_spans_overlap(spans, 6)) return SS_ERR_ARG;
+    const Sizes s(T, V, K);
+    const ForwardPlace place(s);
+    if (scratch_bytes < ss_cross_entropy_scratch_bytes(T, V, K)) return SS_ERR_ARG;
+    char *base = static_cast<char *>(scratch);
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (!loadable(h, K, ldh)) {
+        rc = copied(h, ldh, base + place.h, T, K, s.K64, T, nullptr, stream);
+        if (rc != SS_OK) return rc;
+        h = base + place.h, ldh = s.K64;
+    }
+    const bool copy = !loadable(w, K, ldw);
+    const size_t piece = s.forward(copy);
+    loss::Part *parts = reinterpret_cast<loss::Part *>(base + place.parts);
+    float *picked = reinterpret_cast<float *>(base + place.picked);
+    size_t count = 0;
+    for (size_t v = 0; v < V; v += piece) {
+        const size_t n = std::min(piece, V - v);
+        const void *from = static_cast<const char *>(w) + v * ldw * 2;
+        if (copy) {
+            rc = copied(from, ldw, base + place.w, n, K, s.K64, n, nullptr, stream);
+            if (rc != SS_OK) return rc;
+            from = base + place.w;
+        }
+        const Plan plan = product::plan_of(T, n, s.K64, 1, false);
+        const Product p{Operand{h, (uint32_t)ldh, (uint32_t)T, 0, 0}, Operand{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0}, 1, T, n, s.K64 / product::kStep, nullptr};
+        rc = product::run<product::Bf16, false, false, loss::StatsEnd>(plan, p, {parts, picked, target, (int64_t)v, (uint32_t)count}, stream);
+        if (rc != SS_OK) return rc;
+        count += 2 * tiles_of(n, plan.tile);
+    }
+    uint32_t rows = 1;
+    while (rows < 64 && rows < T) rows *= 2;
+    const loss::JoinArgs join{parts, picked, target, loss, lse, (uint32_t)T, (uint32_t)count, rows, (int64_t)V};
+    return launch(loss::join_stats_kernel, (T + rows - 1) / rows, 0, stream, join, 256);
+}
+
+int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V, size_t K, size_t ldw, const int64_t *target,
+                          const float *lse, const float *dloss, void *dh, ss_dtype dhdt, size_t lddh, void *dw, ss_dtype dwdt, size_t lddw, void *scratch,
+                          size_t scratch_bytes, void *hip_stream) {
+    int rc = check(h, dt, T, ldh, w, V, K, ldw, target);
+    if (rc != SS_OK) return rc;
+    if ((dhdt != SS_F32 && dhdt != SS_BF16) || (dwdt != SS_F32 && dwdt != SS_BF16)) return SS_ERR_DTYPE;
+    if ((dh && bad_ld(lddh, K)) || (dw && bad_ld(lddw, K))) return SS_ERR_ARG;
+    if (T == 0 && !dw) return SS_OK;
+    if (T && (!lse || !scratch || (!dh && !dw))) return SS_ERR_NULL;
+    if (!element_aligned(lse, SS_F32) || !element_aligned(dloss, SS_F32) || !element_aligned(dh, dhdt) || !element_aligned(dw, dwdt) || !aligned16(scratch)) return SS_ERR_ALIGN;
+    Span spans[8] = {matrix(h, T, K, ldh, dt, false), matrix(w, V, K, ldw, dt, false), span(target, T * 8, false), span(lse, T * 4, false), span(dloss, T * 4, false),
+                     matrix(dh, T, K, lddh, dhdt, true), matrix(dw, V, K, lddw, dwdt, true), span(scratch, scratch_bytes, true)};
+    if (written_spans_overlap(spans, 8)) return SS_ERR_ARG;
+    hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    if (T == 0) {
+        const loss::ZeroArgs a{dw, lddw, (uint64_t)V * K, (uint32_t)K, dwdt == SS_BF16};
+        return launch(loss::zero_kernel, std::min((a.size + 255) / 256, (uint64_t)1 << 16), 0, stream, a, 256);
+    }
+    const Sizes s(T, V, K);
+    const BackwardPlace place(s);
+    if (scratch_bytes < ss_cross_entropy_scratch_bytes(T, V, K)) return SS_ERR_ARG;
+    char *base = static_cast<char *>(scratch);
+    float *factor = reinterpret_cast<float *>(base + place.factor), *scale = reinterpret_cast<float *>(base + place.scale);
+    float *sum = reinterpret_cast<float *>(base + place.sum), *parts = reinterpret_cast<float *>(base + place.parts);
+    __bf16 *d = reinterpret_cast<__bf16 *>(base + place.d);
+    rc = launch(loss::factor_kernel, 1, 0, stream, loss::FactorArgs{dloss, target, factor, scale, (int64_t)V, (uint32_t)T, (uint32_t)s.T64}, 1024);
+    if (rc != SS_OK) return rc;
+    rc = copied(h, ldh, base + place.h, T, K, s.K64, s.T64, target, stream);
+    if (rc != SS_OK) return rc;
+    const bool copy = !loadable(w, K, ldw);
+    const size_t piece = s.backward(copy);
+    const uint32_t K64 = (uint32_t)s.K64, T64 = (uint32_t)s.T64;
+    for (size_t v = 0; v < V; v += piece) {
+        const size_t n = std::min(piece, V - v), n64 = rounded(n, 64);
+        const void *from = static_cast<const char *>(w) + v * ldw * 2;
+        if (copy) {
+            rc = copied(from, ldw, base + place.w, n, K, s.K64, n, nullptr, stream);
+            if (rc != SS_OK) return rc;
+            from = base + place.w;
+        }
+        const Operand hs{base + place.h, K64, T64, T64, 0}, ws{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0}, ds{d, (uint32_t)n64, T64, 0, 0};
+        rc = product::run<product::Bf16, false, false, loss::SoftmaxEnd>(product::plan_of(T64, n64, K64, 1, false), {hs, ws, 1, T64, n64, K64 / product::kStep, nullptr},
+                                                                         {lse, factor, target, (int64_t)v, d, (uint32_t)n64, (uint32_t)T, (uint32_t)n}, stream);
+        if (rc != SS_OK) return rc;
+        if (dh) {
+            // the weights lie down their tokens
+            const Operand down{from, ws.ld, (uint32_t)K, (uint32_t)n, 0};
+            rc = product::run<product::Bf16, false, true, loss::GradientEnd>(product::plan_of(T, K, n64, 1, true), {ds, down, 1, T, K, n64 / product::kStep, parts},
+                                                                             {scale, sum, dh, lddh, v == 0, v + piece >= V, dhdt == SS_BF16}, stream);
+            if (rc != SS_OK) return rc;
+        }
+        if (dw) {
+            const Operand d_down{d, (uint32_t)n64, (uint32_t)n64, T64, 0}, h_down{base + place.h, K64, (uint32_t)K, T64, 0};
+            rc = product::run<product::Bf16, true, true, loss::GradientEnd>(
+                product::plan_of(n, K, s.T64, 1, true), {d_down, h_down, 1, n, K, s.T64 / product::kStep, parts},
+                {scale, nullptr, static_cast<char *>(dw) + v * lddw * grad_bytes(dwdt), lddw, true, true, dwdt == SS_BF16}, stream);
+            if (rc != SS_OK) return rc;
+        }
+    }
+    return SS_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,253 @@
+// Softmax cross entropy over a large vocabulary, z = h w^T, and its gradient, neither of which keeps z.
+//
+// Forward: the tiles of z stay in registers; of each row a tile leaves its largest entry m and the sum of exp(z - m), and
+// whoever has the target's column leaves that entry.  One kernel joins them: lse = M + log(sum of s exp(m - M)).
+// Backward: with lse in hand exp(z - lse) is the softmax, so that D = dloss (softmax - target) is computed tile by tile once more, a
+// piece of the vocabulary at a time, rounded to bf16 for the products dh += D w and dw = D^T h.
+#pragma once
+#include "product_kernels.hpp"
+
+#pragma clang fp contract(off)
+
+namespace loss {
+
+using product::f32x16;
+using product::f32x4;
+using product::u32x4;
+
+constexpr float kLog2e = 1.44269504f;
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+
+// ------------------------------------------------------------- forward ----
+
+struct Part {
+    float top, sum;
+};
+
+struct StatsEnd {
+    static constexpr bool kStrips = false;
+    struct Args {
+        Part *parts;               // (half a tile's columns, row)
+        float *picked;             // the target's logit, by row
+        const int64_t *target;
+        int64_t first;             // token of column 0
+        uint32_t part0;            // the first part of this piece
+    };
+    // A wave's 32 T rows by 32 T columns of z; a row is in lanes r and r + 32, four columns of each eight
+    template <int T>
+    static __device__ __forceinline__ void finish(const Args &a, const f32x16 (&c)[T][T], uint32_t m, uint32_t n, uint32_t part, uint32_t M, uint32_t N, uint32_t r, uint32_t q) {
+        const uint32_t left = N > n + 4 * q ? N - n - 4 * q : 0;      // columns from this lane's first one on: a part of none counts for nothing
+#pragma unroll
+        for (int i = 0; i < T; ++i) {
+            const uint32_t row = m + i * 32 + r;
+            const bool there = row < M;
+            float top = -__builtin_inff();
+#pragma unroll
+            for (int k = 0; k < T; ++k)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint32_t col = k * 32 + e / 4 * 8 + e % 4;
+                    if (col < left) top = fmaxf(top, c[i][k][e]);
+                }
+            top = fmaxf(top, __shfl_xor(top, 32));
+            // NaN passes: it is not the largest, but its exponential is NaN
+            float sum = 0;
+#pragma unroll
+            for (int k = 0; k < T; ++k)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const uint32_t col = k * 32 + e / 4 * 8 + e % 4;
+                    const float z = c[i][k][e];
+                    if (col < left) sum += z == -__builtin_inff() ? 0.0f : exp_of(z - top);
+                }
+            sum += __shfl_xor(sum, 32);
+            if (there && q == 0) a.parts[(size_t)(a.part0 + part) * M + row] = Part{top, sum};
+            const int64_t hit = there ? a.target[row] - a.first - n - 4 * q : -1;
+            if (hit >= 0 && hit < 32 * T && hit < left) {
+#pragma unroll
+                for (int k = 0; k < T; ++k)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if ((uint32_t)hit == k * 32 + e / 4 * 8 + e % 4) a.picked[row] = c[i][k][e];
+            }
+        }
+    }
+};
+
+struct JoinArgs {
+    const Part *parts;
+    const float *picked;
+    const int64_t *target;
+    float *loss, *lse;
+    uint32_t T, count, rows;       // rows: of a block, a power of two; 256 / rows threads share one
+    int64_t V;
+};
+
+__device__ __forceinline__ Part joined(Part x, Part y) {
+    if (y.top == -__builtin_inff() && y.sum == 0.0f) return x;
+    if (x.top == -__builtin_inff() && x.sum == 0.0f) return y;
+    const float top = fmaxf(x.top, y.top);
+    return Part{top, x.sum * exp_of(x.top - top) + y.sum * exp_of(y.top - top)};
+}
+
+// the parts of a row, in an order that depends on their number and on T alone
+__global__ __launch_bounds__(256) void join_stats_kernel(const JoinArgs a) {
+    __shared__ Part shared[256];
+    const uint32_t in = threadIdx.x & (a.rows - 1), row = blockIdx.x * a.rows + in, slices = 256 / a.rows;
+    Part s{-__builtin_inff(), 0.0f};
+    if (row < a.T)
+        for (uint32_t k = threadIdx.x / a.rows; k < a.count; k += slices) s = joined(s, a.parts[(size_t)k * a.T + row]);
+    shared[threadIdx.x] = s;
+    __syncthreads();
+    for (uint32_t half = 128; half >= a.rows; half >>= 1) {
+        if (threadIdx.x < half) shared[threadIdx.x] = joined(shared[threadIdx.x], shared[threadIdx.x + half]);
+        __syncthreads();
+    }
+    if (threadIdx.x >= a.rows || row >= a.T) return;
+    s = shared[threadIdx.x];
+    const float lse = s.top + logf(s.sum);
+    const int64_t target = a.target[row];
+    a.lse[row] = lse;
+    a.loss[row] = target < 0 ? 0.0f : target < a.V ? lse - a.picked[row] : __builtin_nanf("");
+}
+
+// ------------------------------------------------------------ backward ----
+
+// D of a row t is scale x factor_t x (softmax - target).  scale is the largest |dloss| of a row with a target and is multiplied in when the
+// gradients are whole: where all rows weigh the same the factors are 1, and the target's entries, softmax - 1, lose next to nothing to
+// bf16, where dloss itself would be off by up to 2^-9 in all rows alike.
+struct FactorArgs {
+    const float *dloss;            // NULL: 1
+    const int64_t *target;
+    float *factor, *scale;
+    int64_t V;
+    uint32_t T, padded;
+};
+
+__global__ __launch_bounds__(1024) void factor_kernel(const FactorArgs a) {
+    __shared__ float tops[16];
+    float top = 0;
+    for (uint32_t t = threadIdx.x; t < a.T; t += 1024) {
+        const float w = a.target[t] < 0 ? 0.0f : a.dloss ? fabsf(a.dloss[t]) : 1.0f;
+        top = fmaxf(top, w);       // not of NaN, which its own row's factor keeps
+    }
+    for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
+    if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = 0;
+    for (int k = 0; k < 16; ++k) top = fmaxf(top, tops[k]);
+    // in the range where neither a factor nor a scale loses bits; 1 where there is nothing to weigh
+    const float scale = top > 0.0f && top < __builtin_inff() ? top : 1.0f;
+    if (threadIdx.x == 0) *a.scale = scale;
+    for (uint32_t t = threadIdx.x; t < a.padded; t += 1024) {
+        float f = 0;
+        if (t < a.T) {
+            const int64_t target = a.target[t];
+            f = target < 0 ? 0.0f : target >= a.V ? __builtin_nanf("") : (a.dloss ? a.dloss[t] : 1.0f) / scale;
+        }
+        a.factor[t] = f;
+    }
+}
+
+// D, whole eights of columns and rows: zero beyond the vocabulary and in rows without a target
+struct SoftmaxEnd {
+    static constexpr bool kStrips = true;
+    struct Args {
+        const float *lse, *factor;
+        const int64_t *target;
+        int64_t first;             // token of column 0
+        __bf16 *d;
+        uint32_t ld, T, vocab;     // vocab: columns there are
+    };
+    static __device__ __forceinline__ void store(const Args &a, uint32_t, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t) {
+        product::bf16x8 o = {};
+        const int64_t target = row < a.T ? a.target[row] : -1;
+        if (target >= 0) {
+            const float lse = a.lse[row], f = a.factor[row];
+            const int64_t hit = target - a.first - col;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const float p = exp_of(v[x / 4][x % 4] - lse);
+                o[x] = (__bf16)(col + x < a.vocab ? f * (hit == x ? p - 1.0f : p) : 0.0f);
+            }
+        }
+        *reinterpret_cast<u32x4 *>(a.d + (size_t)row * a.ld + col) = __builtin_bit_cast(u32x4, o);
+    }
+};
+
+// A gradient, or with the pieces before it the sum so far
+struct GradientEnd {
+    static constexpr bool kStrips = true;
+    struct Args {
+        const float *scale;
+        float *sum;                // rows x N: not wanted where a piece is all there is
+        void *out;
+        uint64_t ld;
+        bool first, last, bf16;
+    };
+    static __device__ __forceinline__ void store(const Args &a, uint32_t, uint32_t row, uint32_t col, f32x4 (&v)[2], uint32_t N) {
+        const uint32_t n = N - col;
+        float *sum = a.sum + (size_t)row * N + col;
+        if (!a.first) {
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x)
+                if (x < n) v[x / 4][x % 4] += sum[x];
+        }
+        if (!a.last) {
+            product::store_eight<float, f32x4>(sum, v, n);
+            return;
+        }
+        const float scale = *a.scale;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x / 4][x % 4] *= scale;
+        product::store_out(a.out, a.bf16, (size_t)row * a.ld + col, v, n);
+    }
+};
+
+// ------------------------------------------------------ operands that are copied ----
+
+// rows x cols elements with zeros around them, rows of `ld` (a multiple of 64) elements from 16-byte aligned memory: an operand that the products can load.
+// Rows without a target become zero, so that whatever a padded batch holds there meets a zero of D as a zero.
+struct CopyArgs {
+    const uint16_t *from;
+    uint16_t *to;
+    const int64_t *target;         // NULL: all rows stay
+    uint64_t ld_from;
+    uint32_t rows, cols, ld, lines;
+    bool wide;                     // from's rows are 16-byte aligned
+};
+
+__global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a) {
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+    const uint32_t across = a.ld / 8;
+    const uint32_t row = (uint32_t)(at / across), col = (uint32_t)(at - (uint64_t)row * across) * 8;
+    if (row >= a.lines) return;
+    u32x4 v = {0, 0, 0, 0};
+    if (row < a.rows && col < a.cols && (!a.target || a.target[row] >= 0)) {
+        const uint16_t *from = a.from + row * a.ld_from + col;
+        if (a.wide && col + 8 <= a.cols) v = *reinterpret_cast<const u32x4 *>(from);
+        else
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x)
+                if (col + x < a.cols) v[x / 2] |= (uint32_t)from[x] << (x % 2 * 16);
+    }
+    *reinterpret_cast<u32x4 *>(a.to + (size_t)row * a.ld + col) = v;
+}
+
+// the gradient of no rows at all
+struct ZeroArgs {
+    void *out;
+    uint64_t ld, size;
+    uint32_t cols;
+    bool bf16;
+};
+
+__global__ __launch_bounds__(256) void zero_kernel(const ZeroArgs a) {
+    for (uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x; at < a.size; at += (uint64_t)gridDim.x * 256) {
+        const uint64_t row = at / a.cols, to = row * a.ld + at - row * a.cols;
+        if (a.bf16) static_cast<uint16_t *>(a.out)[to] = 0;
+        else static_cast<float *>(a.out)[to] = 0;
+    }
+}
+
+}  // namespace loss

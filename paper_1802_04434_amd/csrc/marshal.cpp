@@ -720,13 +720,194 @@ PyObject *mx4_linear(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- the loss over a vocabulary, orthogonalised updates ----
+
+// The device that a call's tensors are on, current until the call is over: where it launches, and whose stream it takes.
+struct OnDevice {
+    int was = -1;
+    explicit OnDevice(int device) {
+        int current = -1;
+        if (hipGetDevice(&current) != hipSuccess || current == device) return;
+        if (hipSetDevice(device) == hipSuccess) was = current;
+    }
+    ~OnDevice() {
+        if (was >= 0) (void)hipSetDevice(was);
+    }
+    OnDevice(const OnDevice &) = delete;
+    OnDevice &operator=(const OnDevice &) = delete;
+};
+
+hipStream_t stream_on(PyObject *o, int device) {
+    return o == Py_None ? c10::hip::getCurrentHIPStream((c10::DeviceIndex)device).stream() : stream_arg(o);
+}
+
+int device_of(PyObject *o, const char *name) {
+    const at::Tensor &t = tensor(o, name);
+    if (!t.is_cuda()) raise_type(name, -1, "must live in device memory");
+    return t.device().index();
+}
+
+void same_device(PyObject *o, int device, const char *name) {
+    if (o != Py_None && device_of(o, name) != device) raise_type(name, -1, "must live on device %d", device);
+}
+
+// work memory: any contiguous bytes
+struct Scratch {
+    void *p;
+    size_t bytes;
+    explicit Scratch(PyObject *o) {
+        const at::Tensor &t = tensor(o, "scratch");
+        if (!t.is_cuda()) raise_type("scratch", -1, "must live in device memory");
+        if (t.scalar_type() != at::kByte) raise_type("scratch", -1, "has dtype %s", at::toString(t.scalar_type()));
+        if (!t.is_contiguous()) raise_type("scratch", -1, "must be contiguous");
+        p = t.data_ptr();
+        bytes = (size_t)t.numel();
+    }
+};
+
+// the head's tensors: (h, w, target), whose shapes have to fit
+struct Head {
+    Matrix h, w;
+    const int64_t *target;
+    int device;
+
+    explicit Head(PyObject *const *a) : h(a[0], "h"), w(a[1], "w"), device(device_of(a[0], "h")) {
+        if (h.dtype != SS_BF16) raise_type("h", -1, "must be bfloat16");
+        if (w.dtype != SS_BF16) raise_type("w", -1, "must be bfloat16");
+        if (w.cols != h.cols) raise_type("w", -1, "must have h's %zu columns, got %zu", h.cols, w.cols);
+        target = (const int64_t *)rows(a[2], kI64, "target");
+        same_device(a[1], device, "w");
+    }
+    // as many elements as h has rows
+    void *rows(PyObject *o, Kind kind, const char *name) const {
+        void *p = dev(o, kind, h.rows, name);
+        if ((size_t)THPVariable_Unpack(o).numel() != h.rows) raise_type(name, -1, "must have h's %zu rows", h.rows);
+        same_device(o, device, name);
+        return p;
+    }
+};
+
+// (h, w, target, loss, lse, scratch, stream)
+PyObject *cross_entropy(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<7>(n, [&] {
+        const Head x(a);
+        float *loss = (float *)x.rows(a[3], kF32, "loss"), *lse = (float *)x.rows(a[4], kF32, "lse");
+        const Scratch scratch(a[5]);
+        same_device(a[5], x.device, "scratch");
+        const OnDevice on(x.device);
+        const hipStream_t s = stream_on(a[6], x.device);
+        return unlocked([&] {
+            return ss_cross_entropy(x.h.p, x.h.dtype, x.h.rows, x.h.ld, x.w.p, x.w.rows, x.h.cols, x.w.ld, x.target, loss, lse, scratch.p, scratch.bytes, s);
+        });
+    });
+}
+
+// (h, w, target, lse, dloss, dh, dw, scratch, stream); dloss, dh, dw may be None
+PyObject *cross_entropy_grad(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<9>(n, [&] {
+        const Head x(a);
+        const float *lse = (const float *)x.rows(a[3], kF32, "lse"), *dloss = a[4] == Py_None ? nullptr : (const float *)x.rows(a[4], kF32, "dloss");
+        Matrix none = x.h;
+        none.p = nullptr;
+        const Matrix dh = a[5] == Py_None ? none : Matrix(a[5], "dh"), dw = a[6] == Py_None ? none : Matrix(a[6], "dw");
+        if (a[5] != Py_None) dh.shape(x.h.rows, x.h.cols, "dh");
+        if (a[6] != Py_None) dw.shape(x.w.rows, x.w.cols, "dw");
+        same_device(a[5], x.device, "dh");
+        same_device(a[6], x.device, "dw");
+        const Scratch scratch(a[7]);
+        same_device(a[7], x.device, "scratch");
+        const OnDevice on(x.device);
+        const hipStream_t s = stream_on(a[8], x.device);
+        return unlocked([&] {
+            return ss_cross_entropy_grad(x.h.p, x.h.dtype, x.h.rows, x.h.ld, x.w.p, x.w.rows, x.h.cols, x.w.ld, x.target, lse, dloss, dh.p, dh.dtype, dh.ld, dw.p, dw.dtype,
+                                         dw.ld, scratch.p, scratch.bytes, s);
+        });
+    });
+}
+
+// a matrix, or a stack of them, the elements of a row side by side
+struct Stack {
+    void *p;
+    ss_dtype dtype;
+    size_t count, rows, cols, ld, apart;
+
+    Stack(PyObject *o, const char *name) {
+        const at::Tensor &t = tensor(o, name);
+        if (!t.is_cuda()) raise_type(name, -1, "must live in device memory");
+        if (!is_kind(t.scalar_type(), kGrad)) raise_type(name, -1, "has dtype %s", at::toString(t.scalar_type()));
+        const int64_t d = t.dim();
+        if (t.layout() != at::kStrided || (d != 2 && d != 3)) raise_type(name, -1, "must have two or three dimensions");
+        count = d == 3 ? (size_t)t.size(0) : 1;
+        rows = (size_t)t.size(d - 2);
+        cols = (size_t)t.size(d - 1);
+        const int64_t row = rows > 1 ? t.stride(d - 2) : (int64_t)cols, whole = (int64_t)((rows ? rows - 1 : 0) * (size_t)(row > 0 ? row : 0) + cols);
+        const int64_t matrix = count > 1 ? t.stride(0) : whole;
+        if ((cols > 1 && t.stride(d - 1) != 1) || row < (int64_t)cols) raise_type(name, -1, "must have the elements of a row side by side");
+        if (matrix < whole) raise_type(name, -1, "must have one matrix after the other");
+        ld = (size_t)row;
+        apart = (size_t)matrix;
+        p = t.data_ptr();
+        dtype = grad_dtype(t.scalar_type());
+    }
+    void like(const Stack &o, const char *name) const {
+        if (count != o.count || rows != o.rows || cols != o.cols) raise_type(name, -1, "must be %zu x %zu x %zu, as g is", o.count, o.rows, o.cols);
+    }
+    // fp32 without gaps
+    float *whole(const Stack &o, const char *name) const {
+        like(o, name);
+        if (dtype != SS_F32) raise_type(name, -1, "must be float32");
+        if (count && rows && cols && ((rows > 1 && ld != cols) || (count > 1 && apart != rows * cols))) raise_type(name, -1, "must be contiguous");
+        return (float *)p;
+    }
+};
+
+// (g, out, scratch, steps, stream)
+PyObject *orthogonalize(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<5>(n, [&] {
+        const Stack g(a[0], "g"), out(a[1], "out");
+        out.like(g, "out");
+        const int device = device_of(a[0], "g");
+        same_device(a[1], device, "out");
+        const Scratch scratch(a[2]);
+        same_device(a[2], device, "scratch");
+        const int steps = int_arg(a[3]);
+        const OnDevice on(device);
+        const hipStream_t s = stream_on(a[4], device);
+        return unlocked([&] {
+            return ss_orthogonalize(g.p, g.dtype, g.count, g.rows, g.cols, g.ld, g.apart, steps, out.p, out.dtype, out.ld, out.apart, scratch.p, scratch.bytes, s);
+        });
+    });
+}
+
+// (g, m, beta, delta, x, scratch, ahead, steps, stream)
+PyObject *orthogonal_step(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return entry<9>(n, [&] {
+        const Stack g(a[0], "g");
+        float *m = Stack(a[1], "m").whole(g, "m"), *x = Stack(a[4], "x").whole(g, "x");
+        const float beta = float_arg(a[2]), delta = float_arg(a[3]);
+        const int device = device_of(a[0], "g");
+        same_device(a[1], device, "m");
+        same_device(a[4], device, "x");
+        const Scratch scratch(a[5]);
+        same_device(a[5], device, "scratch");
+        const int ahead = PyObject_IsTrue(a[6]), steps = int_arg(a[7]);
+        if (ahead < 0) throw PyRaised();
+        const OnDevice on(device);
+        const hipStream_t s = stream_on(a[8], device);
+        return unlocked([&] {
+            return ss_orthogonal_step(g.p, g.dtype, g.count, g.rows, g.cols, g.ld, g.apart, m, beta, ahead, steps, delta, x, scratch.p, scratch.bytes, s);
+        });
+    });
+}
+
 #define SS_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     SS_METHOD(signum_pack), SS_METHOD(majority_vote), SS_METHOD(vote_sum), SS_METHOD(sign_apply), SS_METHOD(sum_apply),
     SS_METHOD(signum_vote_step), SS_METHOD(stream_copy), SS_METHOD(welford_update), SS_METHOD(welford_sigma),
     SS_METHOD(density), SS_METHOD(signum_pack_ternary), SS_METHOD(quorum_vote), SS_METHOD(ternary_apply),
     SS_METHOD(signum_vote_step_ternary), SS_METHOD(grad_norm), SS_METHOD(grad_clip), SS_METHOD(mx4_quantize),
-    SS_METHOD(mx4_dequantize), SS_METHOD(mx4_matmul), SS_METHOD(mx4_linear), {nullptr, nullptr, 0, nullptr}};
+    SS_METHOD(mx4_dequantize), SS_METHOD(mx4_matmul), SS_METHOD(mx4_linear),
+    SS_METHOD(cross_entropy), SS_METHOD(cross_entropy_grad), SS_METHOD(orthogonalize), SS_METHOD(orthogonal_step), {nullptr, nullptr, 0, nullptr}};
 #undef SS_METHOD
 
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_marshal", "torch tensors to the C ABI of libsignsgd.so", -1, kMethods,

@@ -1,0 +1,215 @@
+"""Orthogonalised updates on the GPU against their definition in 64 bits: the distance in the Frobenius norm within the bound of
+their roundings (loss_plain.orthogonal_bound), and exactly known results."""
+import pytest
+import torch
+
+import loss_plain as plain
+import paper_1802_04434_amd as ss
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+NAN = float("nan")
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+# one entry to several tiles, wide, tall and square, both sides of 8, 64, 128 and 256
+SHAPES = [(1, 1), (1, 7), (9, 1), (1, 500), (3, 5), (8, 64), (63, 65), (64, 64), (65, 33), (100, 300), (129, 128), (257, 40), (200, 257), (260, 260), (96, 1100), (700, 130)]
+
+
+def matrix(rows, cols, seed=0, kind="gradient"):
+    gen = torch.Generator().manual_seed(seed * 104729 + rows * 31 + cols)
+    x = torch.randn(rows, cols, generator=gen)
+    if kind == "gradient":
+        rank = max(1, min(rows, cols) // 16)
+        x = 0.3 * x + torch.randn(rows, rank, generator=gen) @ torch.randn(rank, cols, generator=gen) / rank ** 0.5
+    if kind == "singular":
+        rank = max(1, min(rows, cols) // 4)
+        x = torch.randn(rows, rank, generator=gen) @ torch.randn(rank, cols, generator=gen)
+    return x
+
+
+def stacked(xs, dtype, pad=0, offset=0, gap=0):
+    """matrices as slices of one buffer of NaN"""
+    n, (rows, cols) = len(xs), xs[0].shape
+    apart = rows * (cols + pad) + gap
+    buffer = torch.full((offset + n * apart + cols,), NAN, dtype=dtype, device=DEV)
+    view = buffer.as_strided((n, rows, cols), (apart, cols + pad, 1), offset)
+    view.copy_(torch.stack(xs))
+    return view
+
+
+def scratch_for(rows, cols, count=1):
+    return ss.new_orthogonalize_scratch(rows, cols, count).fill_(0xFF)
+
+
+def check(got, g, steps=5, scale=1.0):
+    """got against g orthogonalised; g as the kernel was given it"""
+    want = plain.orthogonalized(g, steps)
+    bound = plain.orthogonal_bound(g, steps)
+    half = {torch.float32: plain.U32, torch.bfloat16: plain.U16}[got.dtype]
+    off = float((got.cpu().double() - want).norm())
+    assert off <= bound + half * float(want.norm()), "off by %.3g, %.3g allowed" % (off, bound + half * float(want.norm()))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_orthogonalize(rows, cols, dtype):
+    xs = [matrix(rows, cols, seed).to(DTYPES[dtype]) for seed in range(2)]
+    for pad, offset, gap, odt in ((0, 0, 0, torch.bfloat16), (3, 1, 5, torch.float32), (8, 8, 64, torch.bfloat16)):
+        g = stacked(xs, DTYPES[dtype], pad, offset, gap)
+        out = stacked([torch.zeros(rows, cols)] * 2, odt, pad, offset, gap)
+        ss.orthogonalize(g, out, scratch_for(rows, cols, 2))
+        for i in range(2):
+            check(out[i], xs[i])
+        buffer = out.as_strided((out.untyped_storage().nbytes() // out.element_size(),), (1,), 0).clone()
+        buffer.as_strided(out.shape, out.stride(), offset).fill_(NAN)
+        assert torch.isnan(buffer).all()                 # around the matrices nothing is written
+
+
+@pytest.mark.parametrize("kind", ["normal", "singular"])
+@pytest.mark.parametrize("rows,cols", [(64, 64), (130, 200), (300, 150)])
+def test_other_spectra(rows, cols, kind):
+    x = matrix(rows, cols, 1, kind)
+    out = torch.empty(rows, cols, device=DEV)
+    ss.orthogonalize(x.to(DEV), out, scratch_for(rows, cols))
+    check(out, x)
+
+
+@pytest.mark.parametrize("steps", [1, 2, 3, 8])
+def test_steps(steps):
+    x = matrix(90, 130, 2)
+    out = torch.empty(90, 130, device=DEV)
+    ss.orthogonalize(x.to(DEV), out, scratch_for(90, 130), steps=steps)
+    check(out, x, steps)
+
+
+@pytest.mark.parametrize("n", [1, 4, 16, 64, 256])
+def test_permutations_stay_what_they_are(n):
+    """of n = 4^k rows, with signs: every entry of X is 2^-k, and each singular value goes its own way as a number does"""
+    gen = torch.Generator().manual_seed(n)
+    order, sign = torch.randperm(n, generator=gen), torch.randint(0, 2, (n,), generator=gen) * 2.0 - 1
+    x = torch.zeros(n, n)
+    x[torch.arange(n), order] = sign * 3.0
+    out = torch.empty(n, n, device=DEV)
+    ss.orthogonalize(x.to(DEV), out, scratch_for(n, n))
+    got = out.cpu().double()
+    s, off = n ** -0.5, 0.0
+    for k in range(5):
+        mu = {3: 0.8, 4: 2.0}.get(k, 0.0)
+        b = plain.B * s ** 2 + plain.C * s ** 4 + mu
+        # hi, A (twice from hi, once its own) and B are rounded
+        ea = 3 * plain.H16 * s * s
+        eb = (abs(plain.B) + 2 * plain.C * s * s) * ea + plain.H16 * abs(b)
+        slope = abs(plain.A + 3 * plain.B * s ** 2 + 5 * plain.C * s ** 4)
+        off = off * slope + eb * s + abs(b) * plain.H16 * s + 16 * plain.U32 * 4
+        s = plain.polynomial(s)
+    assert torch.equal(got != 0, x != 0)
+    assert ((got[torch.arange(n), order] * sign - s).abs() <= off).all()
+
+
+def test_scale_makes_no_difference():
+    x = matrix(70, 90)
+    want = torch.empty(70, 90, device=DEV)
+    ss.orthogonalize(x.to(DEV), want, scratch_for(70, 90))
+    for power in (-120, -60, 60, 110):
+        out = torch.empty(70, 90, device=DEV)
+        ss.orthogonalize((x * 2.0 ** power).to(DEV), out, scratch_for(70, 90))
+        assert torch.equal(out, want), power
+
+
+def test_zeros_infinities_and_nan_stay_in_their_matrix():
+    xs = [matrix(70, 90, s) for s in range(5)]
+    xs[1].zero_()
+    xs[2][3, 4] = float("inf")
+    xs[3][69, 89] = NAN
+    xs[4].fill_(torch.finfo(torch.float32).max)
+    out = torch.empty(5, 70, 90, device=DEV)
+    ss.orthogonalize(torch.stack(xs).to(DEV), out, scratch_for(70, 90, 5))
+    check(out[0], xs[0])
+    check(out[4], torch.ones(70, 90))
+    assert (out[1] == 0).all() and torch.isnan(out[2]).all() and torch.isnan(out[3]).all()
+
+
+@pytest.mark.parametrize("ahead", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("count,rows,cols", [(1, 1, 1), (1, 64, 64), (3, 65, 130), (2, 257, 60), (1, 9, 300)])
+def test_step(count, rows, cols, dtype, ahead):
+    beta, delta = 0.9, 0.03
+    b, omb = torch.tensor(beta, dtype=torch.float32), 1 - torch.tensor(beta, dtype=torch.float32)
+    gen = torch.Generator().manual_seed(rows + cols)
+    m = torch.stack([matrix(rows, cols, 7 + i) for i in range(count)])
+    x = torch.randn(count, rows, cols, generator=gen)
+    flat = torch.full((2 * x.numel() + 3,), NAN, device=DEV)        # parts of larger vectors, at odd places
+    md, xd = flat[1:1 + m.numel()].view(m.shape), flat[2 + m.numel():2 + 2 * m.numel()].view(m.shape)
+    md.copy_(m), xd.copy_(x)
+    scratch = scratch_for(rows, cols, count)
+    for k in range(2):
+        gs = [matrix(rows, cols, 20 + 5 * k + i).to(DTYPES[dtype]) for i in range(count)]
+        g = stacked(gs, DTYPES[dtype], 3, 1, 2)
+        before = xd.cpu().double()
+        ss.orthogonal_step(g, md, beta, delta, xd, scratch, ahead=ahead)
+        wide = torch.stack(gs).float()
+        m = b * m + omb * wide
+        assert torch.equal(md.cpu(), m)                  # momentum as ss_signum_pack rounds it
+        u = b * m + omb * wide if ahead else m
+        for i in range(count):
+            want = before[i] - delta * plain.orthogonalized(u[i])
+            off = float((xd[i].cpu().double() - want).norm())
+            allowed = delta * plain.orthogonal_bound(u[i]) + 3 * plain.U32 * float(want.norm() + before[i].norm())
+            assert off <= allowed, (k, i, off, allowed)
+    assert torch.isnan(flat[[0, 1 + m.numel(), -1]]).all()
+
+
+def test_nothing_to_do():
+    for shape in ((0, 5, 6), (2, 0, 6), (2, 5, 0), (0, 4)):
+        g = torch.empty(shape, device=DEV)
+        scratch = ss.new_orthogonalize_scratch(shape[-2], shape[-1], shape[0] if len(shape) == 3 else 1)
+        ss.orthogonalize(g, torch.empty_like(g), scratch)
+        ss.orthogonal_step(g, torch.empty_like(g), 0.9, 0.1, torch.empty_like(g), scratch)
+
+
+def test_same_bits_on_another_stream_and_in_a_replayed_graph():
+    g = torch.stack([matrix(140, 260, s) for s in range(3)]).to(DEV)
+    scratch = scratch_for(140, 260, 3)
+    m0, x0 = torch.randn_like(g), torch.randn_like(g)
+
+    def eager(g, stream=None):
+        out, m, x = torch.empty_like(g), m0.clone(), x0.clone()
+        ss.orthogonalize(g, out, scratch.fill_(0xFF), stream=stream)
+        ss.orthogonal_step(g, m, 0.9, 0.1, x, scratch, stream=stream)
+        return out, m, x
+
+    want = eager(g)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        again = eager(g)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(want, again))
+    out, m, x = torch.empty_like(g), m0.clone(), x0.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ss.orthogonalize(g, out, scratch)
+        ss.orthogonal_step(g, m, 0.9, 0.1, x, scratch)
+    for seed in range(4):
+        g.copy_(torch.stack([matrix(140, 260, 50 + 3 * seed + s) for s in range(3)]))
+        want = eager(g)
+        out.fill_(NAN), m.copy_(m0), x.copy_(x0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (out, m, x))), seed
+
+
+def test_refusals():
+    g, scratch = torch.randn(2, 30, 40, device=DEV), ss.new_orthogonalize_scratch(30, 40, 2)
+    out, m, x = torch.empty_like(g), torch.empty_like(g), torch.empty_like(g)
+    for bad, what in ((g.half(), "g has dtype"), (g.transpose(1, 2), "side by side"), (g.cpu(), "g must live in device memory"), (g[0, 0], "two or three dimensions"),
+                      (g[:1].expand(2, 30, 40), "one matrix after the other"), (g[:, :29], "out must be 2 x 29 x 40")):
+        with pytest.raises(TypeError, match=what):
+            ss.orthogonalize(bad, out, scratch)
+    with pytest.raises(TypeError, match="m must be float32"):
+        ss.orthogonal_step(g, m.bfloat16(), 0.9, 0.1, x, scratch)
+    with pytest.raises(TypeError, match="x must be contiguous"):
+        ss.orthogonal_step(g[:, :, :39], m[:, :, :39].contiguous(), 0.9, 0.1, x[:, :, :39], scratch)
+    for call in (lambda: ss.orthogonalize(g, out, scratch, steps=0), lambda: ss.orthogonalize(g, out, scratch[:-256]), lambda: ss.orthogonalize(g, g, scratch),
+                 lambda: ss.orthogonal_step(g, m, 0.9, float("inf"), x, scratch), lambda: ss.orthogonal_step(g, m, 0.9, 0.1, m, scratch)):
+        with pytest.raises(ss.SignSGDError, match="SS_ERR_ARG"):
+            call()
