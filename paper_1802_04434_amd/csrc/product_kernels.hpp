@@ -64,6 +64,17 @@ struct TilesArgs {
 template <int N>
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
+// 16 bytes a lane straight into LDS, one lane's behind the other's from `to` on.  Not by the builtin: after one the compiler lets no ds_read_b64_tr_b16 go before all loads into LDS are there, whatever
+// part of it they go to (8192 x 4096 x 8192 with both operands down k 1,191 us).  What a step reads has been waited for with arrived().
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"      // m0 is reserved, but not in use here: no other instruction of these kernels reads it
+__device__ __forceinline__ void load_to_lds(const char *base, size_t behind, uint32_t offset, uint32_t to) {
+    const uint64_t p = reinterpret_cast<uint64_t>(base) + behind;
+    const u32x4 window = {(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, 0xFFFFFFFFu, 0x00020000u};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(window) : "m0");
+}
+#pragma clang diagnostic pop
+
 typedef __attribute__((address_space(3))) void *Lds;
 typedef __attribute__((address_space(3))) i16x4 *LdsFour;
 
@@ -120,7 +131,7 @@ struct Way {
             offset = from[i];
             behind = (size_t)step * kStep * 2;
         }
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ss::window(base, behind, 0xFFFFFFFFu), (Lds)(lds + place + (wave + 4 * i) * 1024), 16, (int)offset, 0, 0, 0);
+        load_to_lds(base, behind, offset, (uint32_t)reinterpret_cast<uintptr_t>((Lds)lds) + place + (wave + 4 * i) * 1024);
     }
     // block i (32 rows) of quarter j (16 of the k): lanes below 32 have k 8 j to 8 j + 7 of the step, the others those 32 further on
     __device__ __forceinline__ u32x4 read(const char *lds, int i, int j, uint32_t place) const {
@@ -143,6 +154,30 @@ template <typename E, int T>
 __device__ __forceinline__ void multiply(f32x16 (&c)[T][T], const Fragments<T> &f, int part) {
 #pragma unroll
     for (int x = part * T / 2; x < (part + 1) * T / 2; ++x) c[x / T][x % T] = E::multiply(f.b[x % T], f.a[x / T], c[x / T][x % T]);
+}
+
+// eight neighbours of a row, rounded to the nearest, ties to even; `n` of them where the row ends
+template <typename E, typename V>
+__device__ __forceinline__ void store_eight(E *to, const f32x4 (&v)[2], uint32_t n) {
+    if (n >= 8) {
+        if constexpr (sizeof(E) == 2) {
+            V o;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) o[x] = (E)v[x / 4][x % 4];
+            *reinterpret_cast<u32x4_16 *>(to) = __builtin_bit_cast(u32x4, o);
+        } else {
+            *reinterpret_cast<f32x4_any *>(to) = v[0];
+            *reinterpret_cast<f32x4_any *>(to + 4) = v[1];
+        }
+    } else {
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x)
+            if (x < n) to[x] = (E)v[x / 4][x % 4];
+    }
+}
+__device__ __forceinline__ void store_out(void *to, bool bf16, size_t at, const f32x4 (&v)[2], uint32_t n) {
+    if (bf16) store_eight<__bf16, bf16x8>(static_cast<__bf16 *>(to) + at, v, n);
+    else store_eight<float, f32x4>(static_cast<float *>(to) + at, v, n);
 }
 
 // Tiles of 2 x 2 waves, each 32 T rows by 32 T columns of the result.  A step is 64 of k, multiplied in four quarters; the fragments of the
@@ -257,12 +292,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
                 if (m >= p.M || col >= p.N) continue;
                 if (p.splits == 1) End::store(p.end, stack, m, col, v, p.N);
                 else {
-                    float *to = p.parts + ((size_t)whole * p.M + m) * p.N + col;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            if (col + 4 * h + x < p.N) to[4 * h + x] = v[h][x];
+                    store_eight<float, f32x4>(p.parts + ((size_t)whole * p.M + m) * p.N + col, v, p.N - col);
                 }
             }
         }
@@ -299,30 +329,6 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs<typename End::
                 if (col + x < p.N) v[x / 4][x % 4] += from[k * size + x];
     }
     End::store(p.end, stack, row, col, v, p.N);
-}
-
-// eight neighbours of a row, rounded to the nearest, ties to even; `n` of them where the row ends
-template <typename E, typename V>
-__device__ __forceinline__ void store_eight(E *to, const f32x4 (&v)[2], uint32_t n) {
-    if (n >= 8) {
-        if constexpr (sizeof(E) == 2) {
-            V o;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) o[x] = (E)v[x / 4][x % 4];
-            *reinterpret_cast<u32x4_16 *>(to) = __builtin_bit_cast(u32x4, o);
-        } else {
-            *reinterpret_cast<f32x4_any *>(to) = v[0];
-            *reinterpret_cast<f32x4_any *>(to + 4) = v[1];
-        }
-    } else {
-#pragma unroll
-        for (uint32_t x = 0; x < 8; ++x)
-            if (x < n) to[x] = (E)v[x / 4][x % 4];
-    }
-}
-__device__ __forceinline__ void store_out(void *to, bool bf16, size_t at, const f32x4 (&v)[2], uint32_t n) {
-    if (bf16) store_eight<__bf16, bf16x8>(static_cast<__bf16 *>(to) + at, v, n);
-    else store_eight<float, f32x4>(static_cast<float *>(to) + at, v, n);
 }
 
 }  // namespace product

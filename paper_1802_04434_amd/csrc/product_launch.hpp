@@ -18,7 +18,34 @@ struct Plan {
     size_t splits;
 };
 
-inline Plan plan_of(size_t, size_t, size_t, size_t, bool) { return Plan{2, 1}; }
+// What a launch takes by its shape, from products of 64 to 8192 squared by 64 to 16384, as they lie and down k alike: us a step of 64 of k with few blocks on the card
+// and with as many as fit, and us a block besides, for its first loads and for writing the result.  Two launches cost 3 us more, and the partial sums their bytes, written, read
+// and joined at 2.5 TB/s.  us by tiles of 256 / 128 / 64 squared: 4096 cubed 103 / 121 / 200, 2048 cubed 40.6 / 21.6 / 30.3, 1024 cubed 23.5 / 9.6 / 6.2.
+inline Plan plan_of(size_t M, size_t N, size_t K, size_t count, bool may_split) {
+    const size_t steps = (K + kStep - 1) / kStep;
+    constexpr struct {
+        int tile;
+        double fit, empty, alone, full, starts, ends;      // empty: blocks a compute unit up to which a step takes as long as alone
+    } kShapes[] = {{4, 1, 0, 0.86, 1.40, 3.0, 6.0}, {2, 2, 0, 0.32, 0.87, 2.5, 2.5}, {1, 4, 1, 0.20, 0.80, 2.2, 1.0}};
+    Plan best{1, 1};
+    double least = 1e300;
+    for (const auto &s : kShapes) {
+        const size_t tiles = tiles_of(M, s.tile) * tiles_of(N, s.tile) * count;
+        // no more parts than fill the card once
+        for (size_t splits = 1; splits == 1 || (may_split && splits * 2 <= steps && tiles * splits <= (size_t)(256 * s.fit)); splits *= 2) {
+            const double blocks = (double)(tiles * splits), each = (double)((steps + splits - 1) / splits);
+            auto round = [&](double load) {       // blocks a compute unit
+                const double crowd = std::fmax(0.0, (load - s.empty) / (s.fit - s.empty));
+                return each * (s.alone + (s.full - s.alone) * crowd) + s.starts + s.ends * std::fmax(0.25, load / s.fit);
+            };
+            const double rounds = std::floor(blocks / (256 * s.fit)), rest = blocks / 256 - rounds * s.fit;
+            double us = rounds * round(s.fit) + (rest > 0 ? round(rest) : 0);
+            if (splits > 1) us += 3.0 + (double)(count * splits * M * N) * 8 / 5e6;
+            if (us < least) least = us, best = Plan{s.tile, splits};
+        }
+    }
+    return best;
+}
 
 // bytes of partial sums
 inline size_t parts_bytes(const Plan &plan, size_t count, size_t M, size_t N) { return plan.splits > 1 ? count * plan.splits * M * N * sizeof(float) : 0; }
@@ -34,7 +61,8 @@ int run(const Plan &plan, const Product &p, const typename End::Args &end, hipSt
     const size_t tiles_m = tiles_of(p.M, plan.tile), tiles_n = tiles_of(p.N, plan.tile), blocks = tiles_m * tiles_n * plan.splits * p.count;
     if (blocks > kMaxBlocks) return SS_ERR_ARG;
     const TilesArgs<typename End::Args> args{p.a, p.b, (uint32_t)p.M, (uint32_t)p.N, (uint32_t)p.steps, (uint32_t)tiles_m, (uint32_t)tiles_n, (uint32_t)plan.splits, p.parts, end};
-    const int rc = host::launch(tiles_kernel<E, A_DOWN, B_DOWN, 2, End>, blocks, 0, stream, args, 256);
+    const auto kernel = plan.tile == 4 ? tiles_kernel<E, A_DOWN, B_DOWN, 4, End> : plan.tile == 2 ? tiles_kernel<E, A_DOWN, B_DOWN, 2, End> : tiles_kernel<E, A_DOWN, B_DOWN, 1, End>;
+    const int rc = host::launch(kernel, blocks, 0, stream, args, 256);
     if (rc != SS_OK || plan.splits == 1) return rc;
     if constexpr (End::kStrips) {
         const uint64_t across = (p.N + 7) / 8, eights = across * p.M * p.count;
