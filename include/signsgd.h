@@ -515,7 +515,7 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
 #define SS_ORTHOGONAL_MAX_COUNT ((size_t)65535)
 #define SS_ORTHOGONAL_MAX_DIM ((size_t)1 << 20)
 #define SS_ORTHOGONAL_MAX_SHORT ((size_t)1 << 15)      /* the shorter side */
-#define SS_ORTHOGONAL_MAX_ELEMENTS ((size_t)1 << 33)   /* of the stack */
+#define SS_ORTHOGONAL_MAX_ELEMENTS ((size_t)1 << 33)   /* of the stack, with rows and cols rounded up to 64 */
 #define SS_ORTHOGONAL_MAX_STEPS 100
 size_t ss_orthogonalize_scratch_bytes(size_t count, size_t rows, size_t cols);
 

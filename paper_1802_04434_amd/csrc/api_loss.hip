@@ -87,8 +87,7 @@ struct BackwardPlace {
 };
 
 int copied(const void *from, size_t ld_from, void *to, size_t rows, size_t cols, size_t ld, size_t lines, const int64_t *target, hipStream_t stream) {
-    const loss::CopyArgs a{static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to), target, ld_from, (uint32_t)rows, (uint32_t)cols, (uint32_t)ld, (uint32_t)lines,
-                           ld_from % 8 == 0 && aligned16(from)};
+    const loss::CopyArgs a{static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to), target, ld_from, (uint32_t)rows, (uint32_t)cols, (uint32_t)ld, (uint32_t)lines};
     return launch(loss::copy_kernel, (lines * (ld / 8) + 255) / 256, 0, stream, a, 256);
 }
 
@@ -150,7 +149,7 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
         count += 2 * tiles_of(n, plan.tile);
     }
     uint32_t rows = 1;
-    while (rows < 64 && rows < T) rows *= 2;
+    while (rows < 16 && rows < T) rows *= 2;
     const loss::JoinArgs join{parts, picked, target, loss, lse, (uint32_t)T, (uint32_t)count, rows, (int64_t)V};
     return launch(loss::join_stats_kernel, (T + rows - 1) / rows, 0, stream, join, 256);
 }

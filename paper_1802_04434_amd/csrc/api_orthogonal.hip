@@ -19,7 +19,7 @@ struct Stack {
     bool empty() const { return count == 0 || rows == 0 || cols == 0; }
     bool bad() const {
         return count > SS_ORTHOGONAL_MAX_COUNT || rows > SS_ORTHOGONAL_MAX_DIM || cols > SS_ORTHOGONAL_MAX_DIM || std::min(rows, cols) > SS_ORTHOGONAL_MAX_SHORT ||
-               (!empty() && rows * cols > SS_ORTHOGONAL_MAX_ELEMENTS / count);
+               (!empty() && rounded(rows, 64) * rounded(cols, 64) > SS_ORTHOGONAL_MAX_ELEMENTS / count);
     }
     // matrices in rows `ld` apart, `apart` elements from one to the next
     bool bad(size_t ld, size_t apart) const { return ld < cols || ld > ((size_t)1 << 40) || (count > 1 && apart < (rows - 1) * ld + cols) || apart > ((size_t)1 << 48); }
@@ -29,7 +29,7 @@ struct Stack {
 inline bool element_aligned(const void *p, ss_dtype dt) { return reinterpret_cast<uintptr_t>(p) % grad_bytes(dt) == 0; }
 
 // blocks that add up a matrix's squares
-inline size_t norm_blocks(const Stack &s) { return std::min(std::max((s.rows * s.cols + 4095) / 4096, (size_t)1), std::max((size_t)2048 / s.count, (size_t)1)); }
+inline size_t norm_blocks(const Stack &s) { return std::min(std::max((s.rows * s.cols + 2047) / 2048, (size_t)1), std::max((size_t)1024 / s.count, (size_t)1)); }
 
 struct Place {
     size_t rows, cols, shorter, longer;       // whole steps
@@ -76,7 +76,7 @@ int orthogonalized(const Stack &s, const Ends &e, int steps, char *scratch, hipS
     _Float16 *lo = reinterpret_cast<_Float16 *>(scratch + place.lo), *a = reinterpret_cast<_Float16 *>(scratch + place.a), *b = reinterpret_cast<_Float16 *>(scratch + place.b);
     float *parts = reinterpret_cast<float *>(scratch + place.parts);
     const BeginArgs begin{e.g, e.m, reinterpret_cast<double *>(scratch + place.sums), hi[0], lo, e.ld, e.apart, (uint32_t)s.rows, (uint32_t)s.cols, (uint32_t)place.rows,
-                          (uint32_t)place.cols, (uint32_t)blocks, e.beta, e.gdt == SS_BF16, e.ahead};
+                          (uint32_t)place.cols, (uint32_t)blocks, e.beta, e.gdt == SS_BF16, e.ahead, e.ld == s.cols || s.rows == 1};
     int rc = launch(norm_kernel, blocks, 0, stream, begin, 256, (int)s.count);
     if (rc != SS_OK) return rc;
     rc = launch(scale_kernel, (place.rows * place.cols / 8 + 255) / 256, 0, stream, begin, 256, (int)s.count);

@@ -84,19 +84,33 @@ struct JoinArgs {
 };
 
 __device__ __forceinline__ Part joined(Part x, Part y) {
-    if (y.top == -__builtin_inff() && y.sum == 0.0f) return x;
-    if (x.top == -__builtin_inff() && x.sum == 0.0f) return y;
     const float top = fmaxf(x.top, y.top);
+    if (top == -__builtin_inff()) return Part{top, x.sum + y.sum};      // 0, or NaN
     return Part{top, x.sum * exp_of(x.top - top) + y.sum * exp_of(y.top - top)};
 }
 
-// the parts of a row, in an order that depends on their number and on T alone
+// The parts of a row, in an order that depends on their number and on T alone; eight loads of a thread are on the way together.  us with 16 rows a block / with 64 and a load at a time: 8192 rows of 1000
+// parts (66 MB) JOIN_LARGE / 134, 301 of 314 JOIN_RAGGED / 30.6.
 __global__ __launch_bounds__(256) void join_stats_kernel(const JoinArgs a) {
     __shared__ Part shared[256];
     const uint32_t in = threadIdx.x & (a.rows - 1), row = blockIdx.x * a.rows + in, slices = 256 / a.rows;
     Part s{-__builtin_inff(), 0.0f};
     if (row < a.T)
-        for (uint32_t k = threadIdx.x / a.rows; k < a.count; k += slices) s = joined(s, a.parts[(size_t)k * a.T + row]);
+        for (uint32_t k = threadIdx.x / a.rows; k < a.count; k += 8 * slices) {
+            Part p[8];
+            float top = -__builtin_inff();
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) {
+                const uint32_t at = k + x * slices;
+                p[x] = at < a.count ? a.parts[(size_t)at * a.T + row] : Part{-__builtin_inff(), 0.0f};
+            }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) top = fmaxf(top, p[x].top);
+            float sum = 0;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) sum += top == -__builtin_inff() ? p[x].sum : p[x].sum * exp_of(p[x].top - top);
+            s = joined(s, Part{top, sum});
+        }
     shared[threadIdx.x] = s;
     __syncthreads();
     for (uint32_t half = 128; half >= a.rows; half >>= 1) {
@@ -214,7 +228,6 @@ struct CopyArgs {
     const int64_t *target;         // NULL: all rows stay
     uint64_t ld_from;
     uint32_t rows, cols, ld, lines;
-    bool wide;                     // from's rows are 16-byte aligned
 };
 
 __global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a) {
@@ -225,7 +238,7 @@ __global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a) {
     u32x4 v = {0, 0, 0, 0};
     if (row < a.rows && col < a.cols && (!a.target || a.target[row] >= 0)) {
         const uint16_t *from = a.from + row * a.ld_from + col;
-        if (a.wide && col + 8 <= a.cols) v = *reinterpret_cast<const u32x4 *>(from);
+        if (col + 8 <= a.cols) v = *reinterpret_cast<const product::u32x4_16 *>(from);
         else
 #pragma unroll
             for (uint32_t x = 0; x < 8; ++x)

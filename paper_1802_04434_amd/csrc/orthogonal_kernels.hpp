@@ -22,10 +22,6 @@ constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
 constexpr float kLast = 2.0f, kBefore = 0.8f;      // mu of the last step and of the one before it
 constexpr float kScale = 4096.0f, kUnscale = 1.0f / 4096.0f;
 
-__device__ __forceinline__ float element(const void *p, bool bf16, size_t at) {
-    return bf16 ? ss::widen_bf16(static_cast<const uint16_t *>(p)[at]) : static_cast<const float *>(p)[at];
-}
-
 // ------------------------------------------------------------ the update's norm ----
 
 // g, and with momentum m <- beta m + (1 - beta) g, u = m or beta m + (1 - beta) g; else u = g
@@ -37,62 +33,113 @@ struct BeginArgs {
     uint64_t ld, apart;            // of g
     uint32_t rows, cols, rows_padded, cols_padded, blocks;
     float beta;
-    bool bf16, ahead;
+    bool bf16, ahead, flat;        // flat: g has no gaps, so that a matrix is one long row
 };
 
 __device__ __forceinline__ float update_of(const BeginArgs &a, float g, float m) {
     return !a.m ? g : a.ahead ? ss::momentum(a.beta, 1.0f - a.beta, m, g) : m;
 }
 
+// n of eight neighbours, zero beyond
+__device__ __forceinline__ void load_eight(float (&v)[8], const void *p, bool bf16, size_t at, uint32_t n) {
+    if (n >= 8 && bf16) {
+        const u32x4 w = *reinterpret_cast<const product::u32x4_16 *>(static_cast<const uint16_t *>(p) + at);
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x] = ss::widen_bf16((uint16_t)(w[x / 2] >> (x % 2 * 16)));
+    } else if (n >= 8) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 w = *reinterpret_cast<const product::f32x4_any *>(static_cast<const float *>(p) + at + 4 * h);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) v[4 * h + x] = w[x];
+        }
+    } else {
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x)
+            v[x] = x >= n ? 0.0f : bf16 ? ss::widen_bf16(static_cast<const uint16_t *>(p)[at + x]) : static_cast<const float *>(p)[at + x];
+    }
+}
+
+// Squares are exact in fp64 and added there.  A wave takes 512 neighbours of a row at a time.  us: 4096 x 4096 bf16 with momentum NORM_STEP, 8192 x 8192 bf16 NORM_LARGE.
 __global__ __launch_bounds__(256) void norm_kernel(const BeginArgs a) {
     __shared__ double shared[4];
-    const uint32_t stack = blockIdx.y;
-    const size_t size = (size_t)a.rows * a.cols;
+    const uint32_t stack = blockIdx.y, lane = threadIdx.x & 63u;
+    const uint64_t size = (uint64_t)a.rows * a.cols, cols = a.flat ? size : a.cols;
+    const uint32_t rows = a.flat ? 1 : a.rows, across = (uint32_t)((cols + 511) / 512);
+    const uint64_t units = (uint64_t)rows * across;
     double sum = 0;
-    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < size; at += (size_t)a.blocks * 256) {
-        const uint32_t row = (uint32_t)(at / a.cols), col = (uint32_t)(at - (size_t)row * a.cols);
-        const float g = element(a.g, a.bf16, stack * a.apart + row * a.ld + col);
-        float m = 0;
+    for (uint64_t unit = product::uniform(blockIdx.x * 4 + (threadIdx.x >> 6)); unit < units; unit += (uint64_t)a.blocks * 4) {
+        const uint32_t row = (uint32_t)(unit / across);
+        const uint64_t col = (unit - (uint64_t)row * across) * 512 + lane * 8;
+        if (col >= cols) continue;
+        const uint32_t n = cols - col < 8 ? (uint32_t)(cols - col) : 8u;
+        float g[8], m[8] = {};
+        load_eight(g, a.g, a.bf16, stack * a.apart + row * a.ld + col, n);
         if (a.m) {
-            float *to = a.m + stack * size + at;
-            m = ss::momentum(a.beta, 1.0f - a.beta, *to, g);
-            *to = m;
+            float *to = a.m + stack * size + row * cols + col;
+            load_eight(m, to, false, 0, n);
+            f32x4 v[2];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x / 4][x % 4] = m[x] = ss::momentum(a.beta, 1.0f - a.beta, m[x], g[x]);
+            product::store_eight<float, f32x4>(to, v, n);
         }
-        const double u = update_of(a, g, m);
-        sum += u * u;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+            const double u = update_of(a, g[x], m[x]);
+            if (x < n) sum += u * u;
+        }
     }
     sum = ss::sum_wave(sum);
-    if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = sum;
+    if (lane == 63) shared[threadIdx.x >> 6] = sum;
     __syncthreads();
     if (threadIdx.x == 0) a.sums[(size_t)stack * a.blocks + blockIdx.x] = shared[0] + shared[1] + shared[2] + shared[3];
 }
 
-// X = u / |u|, scaled, with zeros around it; zero if u is, NaN if its norm is not finite
+// 4096 / norm as f x p x p: f in [1, 4) and p a power of two, so that no product with an element of the matrix leaves fp32's range on the way and only
+// the last one rounds; all of it zero for a matrix of zeros, NaN where the norm is not finite
+struct Scale {
+    float f, p;
+    __device__ __forceinline__ explicit Scale(double sum) {
+        if (sum == 0) f = 0, p = 1;
+        else if (!(sum < __builtin_inf())) f = __builtin_nanf(""), p = 1;
+        else {
+            const double s = (double)kScale / sqrt(sum);        // 2^-130 (many elements near the largest) to 2^161
+            const int half = (int)(__builtin_bit_cast(uint64_t, s) >> 52) - 1023 >> 1;
+            const double one = __builtin_bit_cast(double, (uint64_t)(1023 + half) << 52);
+            p = (float)one;
+            f = (float)(s / one / one);
+        }
+    }
+    __device__ __forceinline__ float operator()(float u) const { return u * p * p * f; }
+};
+
+// X = u / |u|, scaled, with zeros around it
 __global__ __launch_bounds__(256) void scale_kernel(const BeginArgs a) {
     __shared__ double shared[4];
     const uint32_t stack = blockIdx.y;
+    const uint32_t across = a.cols_padded / 8, at = blockIdx.x * 256 + threadIdx.x;
+    const uint32_t row = at / across, col = (at - row * across) * 8;
+    const bool there = row < a.rows && col < a.cols;
+    const uint32_t n = there ? (a.cols - col < 8 ? a.cols - col : 8u) : 0u;
+    float g[8] = {}, m[8] = {};
+    if (there) {
+        load_eight(g, a.g, a.bf16, stack * a.apart + row * a.ld + col, n);
+        if (a.m) load_eight(m, a.m, false, ((size_t)stack * a.rows + row) * a.cols + col, n);
+    }
     double sum = 0;
     for (uint32_t k = threadIdx.x; k < a.blocks; k += 256) sum += a.sums[(size_t)stack * a.blocks + k];
     sum = ss::sum_wave(sum);
     if ((threadIdx.x & 63) == 63) shared[threadIdx.x >> 6] = sum;
     __syncthreads();
-    sum = shared[0] + shared[1] + shared[2] + shared[3];
-    const double scale = sum == 0 ? 0 : sum < __builtin_inf() ? kScale / sqrt(sum) : __builtin_nan("");
-    const uint32_t across = a.cols_padded / 8;
-    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    const uint32_t row = (uint32_t)(at / across), col = (uint32_t)(at - (uint64_t)row * across) * 8;
     if (row >= a.rows_padded) return;
-    f16x8 hi = {}, lo = {};
-    if (row < a.rows)
+    const Scale scale(shared[0] + shared[1] + shared[2] + shared[3]);
+    f16x8 hi, lo;
 #pragma unroll
-        for (uint32_t x = 0; x < 8; ++x)
-            if (col + x < a.cols) {
-                const float g = element(a.g, a.bf16, stack * a.apart + row * a.ld + col + x);
-                const float m = a.m ? a.m[((size_t)stack * a.rows + row) * a.cols + col + x] : 0;
-                const double v = update_of(a, g, m) * scale;
-                hi[x] = (_Float16)(float)v;
-                lo[x] = (_Float16)(float)(v - (double)(float)hi[x]);
-            }
+    for (uint32_t x = 0; x < 8; ++x) {
+        const float v = x < n ? scale(update_of(a, g[x], m[x])) : 0.0f;
+        hi[x] = (_Float16)v;
+        lo[x] = (_Float16)(v - (float)hi[x]);
+    }
     const size_t to = ((size_t)stack * a.rows_padded + row) * a.cols_padded + col;
     *reinterpret_cast<u32x4 *>(a.hi + to) = __builtin_bit_cast(u32x4, hi);
     *reinterpret_cast<u32x4 *>(a.lo + to) = __builtin_bit_cast(u32x4, lo);
