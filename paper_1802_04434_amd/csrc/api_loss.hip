@@ -143,7 +143,7 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
             from = base + place.w;
         }
         const Plan plan = product::plan_of(T, n, s.K64, 1, false);
-        const Product p{Operand{h, (uint32_t)ldh, (uint32_t)T, 0, 0}, Operand{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0}, 1, T, n, s.K64 / product::kStep, nullptr};
+        const Product p{Operand{h, (uint32_t)ldh, (uint32_t)T, 0, 0, 0}, Operand{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0, 0}, 1, T, n, s.K64 / product::kStep, nullptr};
         rc = product::run<product::Bf16, false, false, loss::StatsEnd>(plan, p, {parts, picked, target, (int64_t)v, (uint32_t)count}, stream);
         if (rc != SS_OK) return rc;
         count += 2 * tiles_of(n, plan.tile);
@@ -194,19 +194,19 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
             if (rc != SS_OK) return rc;
             from = base + place.w;
         }
-        const Operand hs{base + place.h, K64, T64, T64, 0}, ws{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0}, ds{d, (uint32_t)n64, T64, 0, 0};
+        const Operand hs{base + place.h, K64, T64, T64, 0, 0}, ws{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0, 0}, ds{d, (uint32_t)n64, T64, 0, 0, 0};
         rc = product::run<product::Bf16, false, false, loss::SoftmaxEnd>(product::plan_of(T64, n64, K64, 1, false), {hs, ws, 1, T64, n64, K64 / product::kStep, nullptr},
                                                                          {lse, factor, target, (int64_t)v, d, (uint32_t)n64, (uint32_t)T, (uint32_t)n}, stream);
         if (rc != SS_OK) return rc;
         if (dh) {
             // the weights lie down their tokens
-            const Operand down{from, ws.ld, (uint32_t)K, (uint32_t)n, 0};
+            const Operand down{from, ws.ld, (uint32_t)K, (uint32_t)n, 0, 0};
             rc = product::run<product::Bf16, false, true, loss::GradientEnd>(product::plan_of(T, K, n64, 1, true), {ds, down, 1, T, K, n64 / product::kStep, parts},
                                                                              {scale, sum, dh, lddh, v == 0, v + piece >= V, dhdt == SS_BF16}, stream);
             if (rc != SS_OK) return rc;
         }
         if (dw) {
-            const Operand d_down{d, (uint32_t)n64, (uint32_t)n64, T64, 0}, h_down{base + place.h, K64, (uint32_t)K, T64, 0};
+            const Operand d_down{d, (uint32_t)n64, (uint32_t)n64, T64, 0, 0}, h_down{base + place.h, K64, (uint32_t)K, T64, 0, 0};
             rc = product::run<product::Bf16, true, true, loss::GradientEnd>(
                 product::plan_of(n, K, s.T64, 1, true), {d_down, h_down, 1, n, K, s.T64 / product::kStep, parts},
                 {scale, nullptr, static_cast<char *>(dw) + v * lddw * grad_bytes(dwdt), lddw, true, true, dwdt == SS_BF16}, stream);

@@ -31,24 +31,41 @@ inline bool element_aligned(const void *p, ss_dtype dt) { return reinterpret_cas
 // blocks that add up a matrix's squares
 inline size_t norm_blocks(const Stack &s) { return std::min(std::max((s.rows * s.cols + 2047) / 2048, (size_t)1), std::max((size_t)1024 / s.count, (size_t)1)); }
 
+// How many of the last steps multiply operands of 22 bits, in three products of 11: where the result is fp32, and the matrix so short that its roundings do not average out.  Off
+// by, of the result's norm, without / with: 40 x 40 1.1e-3 / 1e-4, 257 x 300 FEW_A, 512 squared 6e-4 / 4e-4, 1024 x 2048 4e-4.
+inline int twofold_steps(size_t shorter, bool fp32) { return !fp32 || shorter >= 1024 ? 0 : shorter >= 512 ? 1 : shorter >= 256 ? 2 : 3; }
+
+struct Plans {
+    Plan square, polynomial, update;
+};
+
 struct Place {
     size_t rows, cols, shorter, longer;       // whole steps
-    Plan square, polynomial, update;
-    size_t sums, hi[2], lo, a, b, parts, bytes;
+    Plans once, twofold;
+    size_t sums, hi[2], lo[2], a[2], b[2], parts, bytes;
 
     Place(const Stack &s) {
         rows = rounded(s.rows, 64), cols = rounded(s.cols, 64);
         shorter = std::min(rows, cols), longer = std::max(rows, cols);
-        square = product::plan_of(shorter, shorter, longer, s.count, true);
-        polynomial = product::plan_of(shorter, shorter, shorter, s.count, true);
-        update = product::plan_of(rows, cols, shorter, s.count, true);
+        const bool some = twofold_steps(shorter, true) > 0;
         Layout l;
         sums = l.take(s.count * norm_blocks(s) * sizeof(double));
-        for (size_t &h : hi) h = l.take(s.count * rows * cols * 2);
-        lo = l.take(s.count * rows * cols * 2);
-        a = l.take(s.count * shorter * shorter * 2);
-        b = l.take(s.count * shorter * shorter * 2);
-        parts = l.take(std::max({parts_bytes(square, s.count, shorter, shorter), parts_bytes(polynomial, s.count, shorter, shorter), parts_bytes(update, s.count, rows, cols)}));
+        for (int k = 0; k < 2; ++k) {
+            hi[k] = l.take(s.count * rows * cols * 2);
+            lo[k] = k == 0 || some ? l.take(s.count * rows * cols * 2) : lo[0];      // in place where no product reads it
+            a[k] = k == 0 || some ? l.take(s.count * shorter * shorter * 2) : 0;
+            b[k] = k == 0 || some ? l.take(s.count * shorter * shorter * 2) : 0;
+        }
+        size_t most = 0;
+        for (Plans *p : {&once, &twofold}) {
+            const size_t times = p == &twofold ? 3 : 1;
+            p->square = product::plan_of(shorter, shorter, times * longer, s.count, true, true);
+            p->polynomial = product::plan_of(shorter, shorter, times * shorter, s.count, true, true);
+            p->update = product::plan_of(rows, cols, times * shorter, s.count, true);
+            if (p == &once || some)
+                most = std::max({most, parts_bytes(p->square, s.count, shorter, shorter), parts_bytes(p->polynomial, s.count, shorter, shorter), parts_bytes(p->update, s.count, rows, cols)});
+        }
+        parts = l.take(most);
         bytes = l.bytes;
     }
 };
@@ -68,14 +85,39 @@ struct Ends {
     bool step;
 };
 
+// whether a matrix fits into LDS as it is worked on there
+inline bool fits(const Stack &s) {
+    const size_t shorter = rounded(std::min(s.rows, s.cols), 32), longer = rounded(std::max(s.rows, s.cols), 32);
+    constexpr size_t kTiles = orthogonal::kWholeWaves * orthogonal::kWholeTiles;
+    return shorter <= 128 && longer / 32 * (shorter / 32) <= kTiles && orthogonal::whole_bytes((uint32_t)shorter, (uint32_t)longer) <= orthogonal::kWholeBytes;
+}
+
+// two blocks on a compute unit where its LDS has room for them
+inline auto whole(uint32_t shorter, bool half) {
+    using namespace orthogonal;
+    switch (shorter) {
+        case 32: return half ? whole_kernel<32, kWholeHalf> : whole_kernel<32, kWholeBytes>;
+        case 64: return half ? whole_kernel<64, kWholeHalf> : whole_kernel<64, kWholeBytes>;
+        case 96: return half ? whole_kernel<96, kWholeHalf> : whole_kernel<96, kWholeBytes>;
+        default: return whole_kernel<128, kWholeBytes>;      // A alone has 64 KB, X as much
+    }
+}
+
 int orthogonalized(const Stack &s, const Ends &e, int steps, char *scratch, hipStream_t stream) {
     using namespace orthogonal;
+    if (fits(s)) {
+        const uint32_t rows = (uint32_t)rounded(s.rows, 32), cols = (uint32_t)rounded(s.cols, 32), bytes = whole_bytes(std::min(rows, cols), std::max(rows, cols));
+        const WholeArgs a{{e.g, e.m, nullptr, nullptr, nullptr, e.ld, e.apart, (uint32_t)s.rows, (uint32_t)s.cols, rows, cols, 0, e.beta, e.gdt == SS_BF16, e.ahead, false},
+                          e.out, e.ldo, e.aparto, e.delta, (uint32_t)steps, e.step, e.odt == SS_BF16};
+        const auto kernel = whole(std::min(rows, cols), bytes <= kWholeHalf);
+        return launch(kernel, s.count, 0, stream, a, 64 * kWholeWaves);
+    }
     const Place place(s);
     const size_t blocks = norm_blocks(s);
-    _Float16 *hi[2] = {reinterpret_cast<_Float16 *>(scratch + place.hi[0]), reinterpret_cast<_Float16 *>(scratch + place.hi[1])};
-    _Float16 *lo = reinterpret_cast<_Float16 *>(scratch + place.lo), *a = reinterpret_cast<_Float16 *>(scratch + place.a), *b = reinterpret_cast<_Float16 *>(scratch + place.b);
+    auto half = [&](size_t at) { return reinterpret_cast<_Float16 *>(scratch + at); };
+    _Float16 *hi[2] = {half(place.hi[0]), half(place.hi[1])}, *lo[2] = {half(place.lo[0]), half(place.lo[1])}, *a[2] = {half(place.a[0]), half(place.a[1])}, *b[2] = {half(place.b[0]), half(place.b[1])};
     float *parts = reinterpret_cast<float *>(scratch + place.parts);
-    const BeginArgs begin{e.g, e.m, reinterpret_cast<double *>(scratch + place.sums), hi[0], lo, e.ld, e.apart, (uint32_t)s.rows, (uint32_t)s.cols, (uint32_t)place.rows,
+    const BeginArgs begin{e.g, e.m, reinterpret_cast<double *>(scratch + place.sums), hi[0], lo[0], e.ld, e.apart, (uint32_t)s.rows, (uint32_t)s.cols, (uint32_t)place.rows,
                           (uint32_t)place.cols, (uint32_t)blocks, e.beta, e.gdt == SS_BF16, e.ahead, e.ld == s.cols || s.rows == 1};
     int rc = launch(norm_kernel, blocks, 0, stream, begin, 256, (int)s.count);
     if (rc != SS_OK) return rc;
@@ -84,25 +126,23 @@ int orthogonalized(const Stack &s, const Ends &e, int steps, char *scratch, hipS
     const bool tall = place.rows > place.cols;
     const uint32_t R = (uint32_t)place.rows, C = (uint32_t)place.cols, S = (uint32_t)place.shorter;
     const uint64_t whole = (uint64_t)R * C, square = (uint64_t)S * S;
+    const int precise = twofold_steps(place.shorter, e.odt == SS_F32);
     for (int k = 0; k < steps; ++k) {
-        const bool last = k + 1 == steps;
+        const bool last = k + 1 == steps, twofold = k + precise >= steps;
         const float mu = last ? kLast : k + 2 == steps ? kBefore : 0.0f;
-        const Operand x{hi[k & 1], C, R, R, whole}, as{a, S, S, S, square}, bs{b, S, S, S, square};
-        if (tall) {
-            const Operand down{hi[k & 1], C, C, R, whole};
-            rc = product::run<product::F16, true, true, SquareEnd>(place.square, {down, down, s.count, S, S, R / product::kStep, parts}, {a, square}, stream);
-        } else {
-            rc = product::run<product::F16, false, false, SquareEnd>(place.square, {x, x, s.count, S, S, C / product::kStep, parts}, {a, square}, stream);
-        }
+        const int at = k & 1, next = ~k & 1;
+        const Plans &plans = twofold ? place.twofold : place.once;
+        const Operand x{hi[at], C, R, R, whole, lo[at] - hi[at]}, down{hi[at], C, C, R, whole, lo[at] - hi[at]}, as{a[0], S, S, S, square, a[1] - a[0]}, bs{b[0], S, S, S, square, b[1] - b[0]};
+        _Float16 *const a_lo = twofold ? a[1] : nullptr, *const b_lo = twofold ? b[1] : nullptr;
+        const SquareEnd::Args square_end{a[0], a_lo, square};
+        if (tall) rc = product::run<product::F16, true, true, SquareEnd>(plans.square, {down, down, s.count, S, S, R / product::kStep, parts, twofold}, square_end, stream);
+        else rc = product::run<product::F16, false, false, SquareEnd>(plans.square, {x, x, s.count, S, S, C / product::kStep, parts, twofold}, square_end, stream);
         if (rc != SS_OK) return rc;
-        rc = product::run<product::F16, false, false, PolynomialEnd>(place.polynomial, {as, as, s.count, S, S, S / product::kStep, parts}, {a, b, square, mu}, stream);
+        rc = product::run<product::F16, false, false, PolynomialEnd>(plans.polynomial, {as, as, s.count, S, S, S / product::kStep, parts, twofold}, {a[0], a_lo, b[0], b_lo, square, mu}, stream);
         if (rc != SS_OK) return rc;
-        const UpdateEnd::Args end{hi[k & 1], lo, hi[~k & 1], last ? e.out : nullptr, whole, e.ldo, e.aparto, (uint32_t)s.rows, (uint32_t)s.cols, kA - mu, e.delta, e.step, e.odt == SS_BF16};
-        if (tall) rc = product::run<product::F16, false, false, UpdateEnd>(place.update, {x, bs, s.count, R, C, S / product::kStep, parts}, end, stream);
-        else {
-            const Operand down{hi[k & 1], C, C, R, whole};
-            rc = product::run<product::F16, false, true, UpdateEnd>(place.update, {bs, down, s.count, R, C, S / product::kStep, parts}, end, stream);
-        }
+        const UpdateEnd::Args end{hi[at], lo[at], hi[next], lo[next], last ? e.out : nullptr, whole, e.ldo, e.aparto, (uint32_t)s.rows, (uint32_t)s.cols, kA - mu, e.delta, e.step, e.odt == SS_BF16};
+        if (tall) rc = product::run<product::F16, false, false, UpdateEnd>(plans.update, {x, bs, s.count, R, C, S / product::kStep, parts, twofold}, end, stream);
+        else rc = product::run<product::F16, false, true, UpdateEnd>(plans.update, {bs, down, s.count, R, C, S / product::kStep, parts, twofold}, end, stream);
         if (rc != SS_OK) return rc;
     }
     return SS_OK;

@@ -165,7 +165,7 @@ __global__ __launch_bounds__(1024) void factor_kernel(const FactorArgs a) {
 
 // D, whole eights of columns and rows: zero beyond the vocabulary and in rows without a target
 struct SoftmaxEnd {
-    static constexpr bool kStrips = true;
+    static constexpr bool kStrips = true, kSymmetric = false;
     struct Args {
         const float *lse, *factor;
         const int64_t *target;
@@ -173,25 +173,32 @@ struct SoftmaxEnd {
         __bf16 *d;
         uint32_t ld, T, vocab;     // vocab: columns there are
     };
-    static __device__ __forceinline__ void store(const Args &a, uint32_t, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t) {
-        product::bf16x8 o = {};
-        const int64_t target = row < a.T ? a.target[row] : -1;
-        if (target >= 0) {
-            const float lse = a.lse[row], f = a.factor[row];
-            const int64_t hit = target - a.first - col;
+    struct Besides {
+        float lse, factor;
+        int64_t target;
+    };
+    static __device__ __forceinline__ Besides load(const Args &a, uint32_t, uint32_t row, uint32_t, uint32_t) {
+        return row < a.T ? Besides{a.lse[row], a.factor[row], a.target[row]} : Besides{0, 0, -1};
+    }
+    static __device__ __forceinline__ void finish(const Args &a, const Besides &b, uint32_t, uint32_t col, f32x4 (&v)[2]) {
+        const int64_t hit = b.target - a.first - col;
 #pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                const float p = exp_of(v[x / 4][x % 4] - lse);
-                o[x] = (__bf16)(col + x < a.vocab ? f * (hit == x ? p - 1.0f : p) : 0.0f);
-            }
+        for (int x = 0; x < 8; ++x) {
+            const float p = exp_of(v[x / 4][x % 4] - b.lse);
+            v[x / 4][x % 4] = b.target >= 0 && col + x < a.vocab ? b.factor * (hit == x ? p - 1.0f : p) : 0.0f;
         }
+    }
+    static __device__ __forceinline__ void put(const Args &a, uint32_t, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t) {
+        product::bf16x8 o;
+#pragma unroll
+        for (int x = 0; x < 8; ++x) o[x] = (__bf16)v[x / 4][x % 4];
         *reinterpret_cast<u32x4 *>(a.d + (size_t)row * a.ld + col) = __builtin_bit_cast(u32x4, o);
     }
 };
 
 // A gradient, or with the pieces before it the sum so far
 struct GradientEnd {
-    static constexpr bool kStrips = true;
+    static constexpr bool kStrips = true, kSymmetric = false;
     struct Args {
         const float *scale;
         float *sum;                // rows x N: not wanted where a piece is all there is
@@ -199,16 +206,27 @@ struct GradientEnd {
         uint64_t ld;
         bool first, last, bf16;
     };
-    static __device__ __forceinline__ void store(const Args &a, uint32_t, uint32_t row, uint32_t col, f32x4 (&v)[2], uint32_t N) {
-        const uint32_t n = N - col;
-        float *sum = a.sum + (size_t)row * N + col;
-        if (!a.first) {
+    struct Besides {
+        f32x4 v[2];
+    };
+    static __device__ __forceinline__ Besides load(const Args &a, uint32_t, uint32_t row, uint32_t col, uint32_t N) {
+        Besides b = {};
+        if (a.first) return b;
+        const float *sum = a.sum + (size_t)row * N + col;
+        if (N - col >= 8)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b.v[h] = *reinterpret_cast<const product::f32x4_any *>(sum + 4 * h);
+        else
 #pragma unroll
             for (uint32_t x = 0; x < 8; ++x)
-                if (x < n) v[x / 4][x % 4] += sum[x];
-        }
+                if (col + x < N) b.v[x / 4][x % 4] = sum[x];
+        return b;
+    }
+    static __device__ __forceinline__ void finish(const Args &, const Besides &b, uint32_t, uint32_t, f32x4 (&v)[2]) { v[0] += b.v[0], v[1] += b.v[1]; }
+    static __device__ __forceinline__ void put(const Args &a, uint32_t, uint32_t row, uint32_t col, f32x4 (&v)[2], uint32_t N) {
+        const uint32_t n = N - col;
         if (!a.last) {
-            product::store_eight<float, f32x4>(sum, v, n);
+            product::store_eight<float, f32x4>(a.sum + (size_t)row * N + col, v, n);
             return;
         }
         const float scale = *a.scale;

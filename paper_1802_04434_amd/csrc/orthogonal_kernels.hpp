@@ -15,6 +15,7 @@
 namespace orthogonal {
 
 using product::f16x8;
+using product::f32x16;
 using product::f32x4;
 using product::u32x4;
 
@@ -104,7 +105,7 @@ struct Scale {
         else if (!(sum < __builtin_inf())) f = __builtin_nanf(""), p = 1;
         else {
             const double s = (double)kScale / sqrt(sum);        // 2^-130 (many elements near the largest) to 2^161
-            const int half = (int)(__builtin_bit_cast(uint64_t, s) >> 52) - 1023 >> 1;
+            const int half = ((int)(__builtin_bit_cast(uint64_t, s) >> 52) - 1023) >> 1;
             const double one = __builtin_bit_cast(double, (uint64_t)(1023 + half) << 52);
             p = (float)one;
             f = (float)(s / one / one);
@@ -147,50 +148,81 @@ __global__ __launch_bounds__(256) void scale_kernel(const BeginArgs a) {
 
 // ------------------------------------------------------------ what becomes of a product ----
 
+// eight neighbours as hi, and lo where it is wanted
+__device__ __forceinline__ void put_eight(_Float16 *hi, _Float16 *lo, size_t at, const f32x4 (&v)[2]) {
+    f16x8 h;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) h[x] = (_Float16)v[x / 4][x % 4];
+    *reinterpret_cast<u32x4 *>(hi + at) = __builtin_bit_cast(u32x4, h);
+    if (!lo) return;
+    f16x8 l;
+#pragma unroll
+    for (int x = 0; x < 8; ++x) l[x] = (_Float16)(v[x / 4][x % 4] - (float)h[x]);
+    *reinterpret_cast<u32x4 *>(lo + at) = __builtin_bit_cast(u32x4, l);
+}
+struct Eight {
+    u32x4 hi, lo;
+};
+__device__ __forceinline__ Eight load_halves(const _Float16 *hi, const _Float16 *lo, size_t at) {
+    return Eight{*reinterpret_cast<const u32x4 *>(hi + at), lo ? *reinterpret_cast<const u32x4 *>(lo + at) : u32x4{0, 0, 0, 0}};
+}
+__device__ __forceinline__ void sum_halves(f32x4 (&v)[2], const Eight &e) {
+    const f16x8 h = __builtin_bit_cast(f16x8, e.hi), l = __builtin_bit_cast(f16x8, e.lo);
+#pragma unroll
+    for (int x = 0; x < 8; ++x) v[x / 4][x % 4] = (float)h[x] + (float)l[x];
+}
+
 // A = X X', from sums that are scaled twice
 struct SquareEnd {
-    static constexpr bool kStrips = true;
+    static constexpr bool kStrips = true, kSymmetric = true;
     struct Args {
-        _Float16 *out;
+        _Float16 *hi, *lo;
         uint64_t apart;
     };
-    static __device__ __forceinline__ void store(const Args &a, uint32_t stack, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t N) {
-        f16x8 o;
+    typedef product::None Besides;
+    static __device__ __forceinline__ Besides load(const Args &, uint32_t, uint32_t, uint32_t, uint32_t) { return {}; }
+    static __device__ __forceinline__ void finish(const Args &, const Besides &, uint32_t, uint32_t, f32x4 (&v)[2]) {
 #pragma unroll
-        for (int x = 0; x < 8; ++x) o[x] = (_Float16)(v[x / 4][x % 4] * kUnscale);
-        *reinterpret_cast<u32x4 *>(a.out + stack * a.apart + (size_t)row * N + col) = __builtin_bit_cast(u32x4, o);
+        for (int x = 0; x < 8; ++x) v[x / 4][x % 4] *= kUnscale;
+    }
+    static __device__ __forceinline__ void put(const Args &a, uint32_t stack, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t N) {
+        put_eight(a.hi, a.lo, stack * a.apart + (size_t)row * N + col, v);
     }
 };
 
 // B + mu I = b A + c A A + mu I
 struct PolynomialEnd {
-    static constexpr bool kStrips = true;
+    static constexpr bool kStrips = true, kSymmetric = true;
     struct Args {
-        const _Float16 *a;
-        _Float16 *out;
+        const _Float16 *a_hi, *a_lo;
+        _Float16 *hi, *lo;
         uint64_t apart;
         float mu;
     };
-    static __device__ __forceinline__ void store(const Args &a, uint32_t stack, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t N) {
-        const size_t at = stack * a.apart + (size_t)row * N + col;
-        const f16x8 was = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(a.a + at));
-        f16x8 o;
+    typedef Eight Besides;
+    static __device__ __forceinline__ Besides load(const Args &a, uint32_t stack, uint32_t row, uint32_t col, uint32_t N) {
+        return load_halves(a.a_hi, a.a_lo, stack * a.apart + (size_t)row * N + col);
+    }
+    static __device__ __forceinline__ void finish(const Args &a, const Besides &besides, uint32_t row, uint32_t col, f32x4 (&v)[2]) {
+        f32x4 was[2];
+        sum_halves(was, besides);
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
-            float s = kB * (float)was[x] + kC * (v[x / 4][x % 4] * kUnscale);
-            if (row == col + x) s += a.mu * kScale;
-            o[x] = (_Float16)s;
+            v[x / 4][x % 4] = kB * was[x / 4][x % 4] + kC * (v[x / 4][x % 4] * kUnscale);
+            if (row == col + x) v[x / 4][x % 4] += a.mu * kScale;
         }
-        *reinterpret_cast<u32x4 *>(a.out + at) = __builtin_bit_cast(u32x4, o);
+    }
+    static __device__ __forceinline__ void put(const Args &a, uint32_t stack, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t N) {
+        put_eight(a.hi, a.lo, stack * a.apart + (size_t)row * N + col, v);
     }
 };
 
 // X <- (a - mu) X + (B + mu I) X; the last time into the result, or off the parameters
 struct UpdateEnd {
-    static constexpr bool kStrips = true;
+    static constexpr bool kStrips = true, kSymmetric = false;
     struct Args {
-        const _Float16 *hi;
-        _Float16 *lo, *hi_out;     // lo in place
+        const _Float16 *hi, *lo;
+        _Float16 *hi_out, *lo_out;
         void *out;                 // NULL: not the last time
         uint64_t apart, ld, out_apart;
         uint32_t rows, cols;       // of the result
@@ -198,21 +230,19 @@ struct UpdateEnd {
         float delta;               // out <- out - delta X where `step`
         bool step, bf16;
     };
-    static __device__ __forceinline__ void store(const Args &a, uint32_t stack, uint32_t row, uint32_t col, f32x4 (&v)[2], uint32_t N) {
-        const size_t at = stack * a.apart + (size_t)row * N + col;
-        const f16x8 hi = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(a.hi + at));
-        const f16x8 lo = __builtin_bit_cast(f16x8, *reinterpret_cast<const u32x4 *>(a.lo + at));
+    typedef Eight Besides;
+    static __device__ __forceinline__ Besides load(const Args &a, uint32_t stack, uint32_t row, uint32_t col, uint32_t N) {
+        return load_halves(a.hi, a.lo, stack * a.apart + (size_t)row * N + col);
+    }
+    static __device__ __forceinline__ void finish(const Args &a, const Besides &besides, uint32_t, uint32_t, f32x4 (&v)[2]) {
+        f32x4 was[2];
+        sum_halves(was, besides);
 #pragma unroll
-        for (int x = 0; x < 8; ++x) v[x / 4][x % 4] = a.factor * ((float)hi[x] + (float)lo[x]) + v[x / 4][x % 4] * kUnscale;
+        for (int x = 0; x < 8; ++x) v[x / 4][x % 4] = a.factor * was[x / 4][x % 4] + v[x / 4][x % 4] * kUnscale;
+    }
+    static __device__ __forceinline__ void put(const Args &a, uint32_t stack, uint32_t row, uint32_t col, f32x4 (&v)[2], uint32_t N) {
         if (!a.out) {
-            f16x8 h, l;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-                h[x] = (_Float16)v[x / 4][x % 4];
-                l[x] = (_Float16)(v[x / 4][x % 4] - (float)h[x]);
-            }
-            *reinterpret_cast<u32x4 *>(a.hi_out + at) = __builtin_bit_cast(u32x4, h);
-            *reinterpret_cast<u32x4 *>(a.lo + at) = __builtin_bit_cast(u32x4, l);
+            put_eight(a.hi_out, a.lo_out, stack * a.apart + (size_t)row * N + col, v);
             return;
         }
         if (row >= a.rows || col >= a.cols) return;
@@ -229,5 +259,224 @@ struct UpdateEnd {
         product::store_out(a.out, a.bf16, to, v, n);
     }
 };
+
+// ------------------------------------------------------------ small matrices, whole ----
+
+// A matrix that fits into LDS with A beside it takes one block and one launch: 64 x 64 SMALL_TINY us (WAS_TINY in the launches of the products above), 120 x 120 SMALL_MID.  X lies as
+// `longer` rows of `shorter` entries, whichever way round g does; both X and A are held in 22 bits, as hi + lo, and products are hi hi + hi lo + lo hi, which costs little here: what bounds
+// it is the way from one product to the next, through LDS and a barrier.
+struct WholeArgs {
+    BeginArgs begin;
+    void *out;
+    uint64_t ld, apart;
+    float delta;
+    uint32_t steps;
+    bool step, bf16;
+};
+
+constexpr int kWholeWaves = 16, kWholeTiles = 2;     // tiles of 32 squared that a wave may have to itself
+constexpr int kWholeUnits = 4;                       // eights of a row that a thread brings: 32 tiles have no more
+constexpr uint32_t kWholeBytes = 160 * 1024 - 256, kWholeHalf = 80 * 1024 - 256;
+
+__host__ __device__ constexpr uint32_t whole_bytes(uint32_t shorter, uint32_t longer) { return 4 * (shorter + longer) * shorter; }
+
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+// Rows of S (32, 64, 96 or 128) entries in LDS.  Chunk c (eight entries) of row r lies at place c ^ x(r), so that neither 16 rows' same chunk nor four rows' four
+// neighbouring chunks share a bank: the first is what a read along the rows takes at a time, the second one down them.
+template <uint32_t S>
+__device__ __forceinline__ uint32_t place(uint32_t row, uint32_t col) {
+    const uint32_t x = (row >> 2 & 3u) ^ (S == 128 ? (row & 3u) << 2 : S == 64 ? (row & 2u) << 1 : 0u);
+    return row * S * 2 + (((col >> 3) ^ x) << 4) + (col & 7u) * 2;
+}
+
+// eight neighbouring k of a row
+template <uint32_t S>
+__device__ __forceinline__ u32x4 along(const char *p, uint32_t row, uint32_t k, uint32_t lane) {
+    return *reinterpret_cast<const u32x4 *>(p + place<S>(row + (lane & 31u), k + (lane >> 5) * 8));
+}
+// the same of a column, for k that lies down
+template <uint32_t S>
+__device__ __forceinline__ u32x4 down(const char *p, uint32_t col, uint32_t k, uint32_t lane) {
+    const uint32_t t = lane & 15u, row = k + (lane >> 5) * 8 + (t >> 2), at = col + (lane >> 4 & 1u) * 16 + (t & 3u) * 4;
+    typedef product::u32x2 u32x2;
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((product::LdsFour)(p + place<S>(row, at))));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((product::LdsFour)(p + place<S>(row + 4, at))));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+}
+
+// A tile of 32 squared: 32 rows (or columns, DOWN) from m on of one matrix with those from n on of the other, over `depth` (a multiple of 32).  Two sums, so that a
+// multiplication seldom waits for the one before it, and the fragments of two steps on the way together.
+template <uint32_t S, bool DOWN>
+__device__ __forceinline__ f32x16 whole_tile(const char *mh, const char *ml, uint32_t m, const char *nh, const char *nl, uint32_t n, uint32_t depth, uint32_t lane) {
+    f32x16 s = {}, t = {};
+    auto read = [&](const char *p, uint32_t at, uint32_t k) { return DOWN ? down<S>(p, at, k, lane) : along<S>(p, at, k, lane); };
+    auto multiply = [&](uint32_t k) {
+        u32x4 f[2][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) f[h][0] = read(nh, n, k + 16 * h), f[h][1] = read(mh, m, k + 16 * h), f[h][2] = read(ml, m, k + 16 * h), f[h][3] = read(nl, n, k + 16 * h);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            s = product::F16::multiply(f[h][0], f[h][1], s);
+            t = product::F16::multiply(f[h][0], f[h][2], t);
+            t = product::F16::multiply(f[h][3], f[h][1], t);
+        }
+    };
+    if constexpr (DOWN) {
+        for (uint32_t k = 0; k < depth; k += 32) multiply(k);
+    } else {
+#pragma unroll 2
+        for (uint32_t k = 0; k < S; k += 32) multiply(k);
+    }
+    return s + t;
+}
+
+// four neighbours as hi + lo
+__device__ __forceinline__ void put_four(char *hi, char *lo, uint32_t at, const f32x4 &v) {
+    f16x4 h, l;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) h[x] = (_Float16)v[x], l[x] = (_Float16)(v[x] - (float)h[x]);
+    *reinterpret_cast<f16x4 *>(hi + at) = h;
+    *reinterpret_cast<f16x4 *>(lo + at) = l;
+}
+__device__ __forceinline__ f32x4 get_four(const char *hi, const char *lo, uint32_t at) {
+    const f16x4 h = *reinterpret_cast<const f16x4 *>(hi + at), l = *reinterpret_cast<const f16x4 *>(lo + at);
+    return f32x4{(float)h[0] + (float)l[0], (float)h[1] + (float)l[1], (float)h[2] + (float)l[2], (float)h[3] + (float)l[3]};
+}
+
+template <uint32_t S, uint32_t BYTES>
+__global__ __launch_bounds__(64 * kWholeWaves) void whole_kernel(const WholeArgs p) {
+    __shared__ __attribute__((aligned(16))) char lds[BYTES];
+    __shared__ double shared[kWholeWaves];
+    constexpr uint32_t kThreads = 64 * kWholeWaves;
+    const BeginArgs &a = p.begin;
+    const uint32_t stack = blockIdx.x, lane = threadIdx.x & 63u, wave = product::uniform(threadIdx.x >> 6), r = lane & 31u, q = lane >> 5;
+    const bool tall = a.rows > a.cols;
+    const uint32_t longer = tall ? a.rows_padded : a.cols_padded;
+    char *const xh = lds, *const xl = xh + longer * S * 2, *const ah = xl + longer * S * 2, *const al = ah + S * S * 2;
+    // eights of a row, kept in registers: all loads are on the way together
+    const uint32_t size = a.rows * a.cols, eights = (a.cols + 7) / 8, units = a.rows * eights;
+    float u[kWholeUnits][8];
+    double sum = 0;
+#pragma unroll
+    for (int k = 0; k < kWholeUnits; ++k) {
+        const uint32_t unit = threadIdx.x + k * kThreads, row = unit / eights, col = (unit - row * eights) * 8;
+        if (unit < units) load_eight(u[k], a.g, a.bf16, stack * a.apart + row * a.ld + col, a.cols - col);
+        else
+#pragma unroll
+            for (int x = 0; x < 8; ++x) u[k][x] = 0;
+    }
+    if (a.m) {
+#pragma unroll
+        for (int k = 0; k < kWholeUnits; ++k) {
+            const uint32_t unit = threadIdx.x + k * kThreads, row = unit / eights, col = (unit - row * eights) * 8;
+            if (unit >= units) break;
+            float *to = a.m + (size_t)stack * size + row * a.cols + col;
+            float m[8];
+            load_eight(m, to, false, 0, a.cols - col);
+            f32x4 v[2];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                v[x / 4][x % 4] = m[x] = ss::momentum(a.beta, 1.0f - a.beta, m[x], u[k][x]);
+                u[k][x] = update_of(a, u[k][x], m[x]);
+            }
+            product::store_eight<float, f32x4>(to, v, a.cols - col);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kWholeUnits; ++k)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) sum += (double)u[k][x] * (double)u[k][x];     // zero beyond a row
+    sum = ss::sum_wave(sum);
+    if (lane == 63) shared[wave] = sum;
+    for (uint32_t at = threadIdx.x * 16; at < 4 * longer * S; at += kThreads * 16) *reinterpret_cast<u32x4 *>(lds + at) = u32x4{0, 0, 0, 0};
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int k = 0; k < kWholeWaves; ++k) sum += shared[k];
+    const Scale scale(sum);
+#pragma unroll
+    for (int k = 0; k < kWholeUnits; ++k) {
+        const uint32_t unit = threadIdx.x + k * kThreads, row = unit / eights, col = (unit - row * eights) * 8;
+        if (unit >= units) break;
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x) {
+            if (col + x >= a.cols) break;
+            const float v = scale(u[k][x]);
+            const uint32_t to = tall ? place<S>(row, col + x) : place<S>(col + x, row);
+            const _Float16 h = (_Float16)v;
+            *reinterpret_cast<_Float16 *>(xh + to) = h;
+            *reinterpret_cast<_Float16 *>(xl + to) = (_Float16)(v - (float)h);
+        }
+    }
+    __syncthreads();
+    constexpr uint32_t across = S / 32, squares = across * across;
+    const uint32_t tiles = longer / 32 * across;
+    for (uint32_t step = 0; step < p.steps; ++step) {
+        const float mu = step + 1 == p.steps ? kLast : step + 2 == p.steps ? kBefore : 0.0f;
+        // A = X'X
+        if (wave < squares) {
+            const uint32_t m = wave / across * 32, n = wave % across * 32;
+            const f32x16 s = whole_tile<S, true>(xh, xl, m, xh, xl, n, longer, lane);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                put_four(ah, al, place<S>(m + r, n + 8 * e + 4 * q), f32x4{s[4 * e], s[4 * e + 1], s[4 * e + 2], s[4 * e + 3]} * kUnscale);
+        }
+        __syncthreads();
+        // B + mu I = b A + c A A + mu I, in A's place, and then X <- (a - mu) X + X (B + mu I)
+#pragma unroll 1
+        for (int x_too = 0; x_too < 2; ++x_too) {
+            char *const ph = x_too ? xh : ah, *const pl = x_too ? xl : al;
+            const uint32_t count = x_too ? tiles : squares;
+            const float was_by = x_too ? kA - mu : kB, sum_by = x_too ? kUnscale : kC * kUnscale, diagonal = x_too ? 0.0f : mu * kScale;
+            f32x16 c[kWholeTiles];
+#pragma unroll
+            for (int i = 0; i < kWholeTiles; ++i) {
+                const uint32_t tile = wave + i * kWholeWaves, m = tile / across * 32, n = tile % across * 32;
+                if (tile >= count) break;
+                c[i] = whole_tile<S, false>(ph, pl, m, ah, al, n, S, lane);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 was = get_four(ph, pl, place<S>(m + r, n + 8 * e + 4 * q));
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) c[i][4 * e + x] = __builtin_fmaf(was_by, was[x], c[i][4 * e + x] * sum_by);
+                }
+                if (m == n && diagonal != 0.0f)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (r == e / 4 * 8 + 4 * q + e % 4) c[i][e] += diagonal;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < kWholeTiles; ++i) {
+                const uint32_t tile = wave + i * kWholeWaves, m = tile / across * 32, n = tile % across * 32;
+                if (tile >= count) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    put_four(ph, pl, place<S>(m + r, n + 8 * e + 4 * q), f32x4{c[i][4 * e], c[i][4 * e + 1], c[i][4 * e + 2], c[i][4 * e + 3]});
+            }
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < kWholeUnits; ++k) {
+        const uint32_t unit = threadIdx.x + k * kThreads, row = unit / eights, col = (unit - row * eights) * 8, n = a.cols - col;
+        if (unit >= units) break;
+        f32x4 v[2];
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x) {
+            const uint32_t at = x >= n ? 0 : tall ? place<S>(row, col + x) : place<S>(col + x, row);
+            v[x / 4][x % 4] = ((float)*reinterpret_cast<const _Float16 *>(xh + at) + (float)*reinterpret_cast<const _Float16 *>(xl + at)) * kUnscale;
+        }
+        const size_t to = stack * p.apart + row * p.ld + col;
+        if (p.step) {
+            float was[8];
+            load_eight(was, p.out, false, to, n);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x / 4][x % 4] = was[x] - p.delta * v[x / 4][x % 4];
+        }
+        product::store_out(p.out, p.bf16, to, v, n);
+    }
+}
 
 }  // namespace orthogonal

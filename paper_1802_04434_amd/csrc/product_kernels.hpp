@@ -47,15 +47,26 @@ struct Operand {
     uint32_t rows;       // m there are: those beyond read as the last one, or what lies behind it in its 16 bytes
     uint32_t depth;      // k there are, of an operand that lies down: those beyond read as the last one.  Along k there are whole steps.
     uint64_t apart;      // elements from one matrix of a stack to the next
+    int64_t lo;          // of an operand that is the sum of two: elements from one to the other
 };
+
+constexpr uint32_t kHigh = 4;      // tile rows of a band, in which tiles are taken column by column
+
+// tiles of the first `bands` bands of a square of n tiles a side that begin at the diagonal, and the few below it in each band's first columns
+__host__ __device__ constexpr uint32_t half_tiles(uint32_t n, uint32_t bands) {
+    const uint32_t whole = bands * kHigh <= n ? bands : n / kHigh, rest = n - whole * kHigh;
+    return kHigh * (whole * n - kHigh * (whole * (whole - (whole > 0)) / 2)) + (bands > whole ? rest * rest : 0);
+}
 
 template <typename EndArgs>
 struct TilesArgs {
     Operand a, b;
     uint32_t M, N;                    // of the result
     uint32_t steps;
+    uint32_t once;                    // steps of one product.  Operands that are sums of two take three: first times first, A's second times first, first times B's second.
     uint32_t tiles_m, tiles_n;
     uint32_t splits;                  // of k
+    uint32_t bands;                   // of a symmetric result, of which only the tiles on and above the diagonal are computed, each written twice; 0: all of them
     float *parts;                     // the partial sums, if splits > 1: (stack, split, M, N)
     EndArgs end;
 };
@@ -119,17 +130,17 @@ struct Way {
             for (int j = 0; j < 4; ++j) at[j] = (mine + r) * kRow + (((4 * q + j) ^ (r >> 1 & 7u)) * 16);
         }
     }
-    __device__ __forceinline__ void fetch(char *lds, int i, uint32_t place, uint32_t step, uint32_t wave) const {
+    __device__ __forceinline__ void fetch(char *lds, int i, uint32_t place, uint32_t step, int64_t lo, uint32_t wave) const {
         uint32_t offset;
         size_t behind;
         if constexpr (DOWN) {
             const uint32_t left = depth - 1 - step * kStep, last = (left < kStep - 1 ? left : kStep - 1) * ld_bytes;
             const uint32_t k = from[0] + 4 * i * kPerLoad * ld_bytes;
             offset = (k < last ? k : last) + from[1];
-            behind = (size_t)step * kStep * ld_bytes;
+            behind = (size_t)step * kStep * ld_bytes + lo;
         } else {
             offset = from[i];
-            behind = (size_t)step * kStep * 2;
+            behind = (size_t)step * kStep * 2 + lo;
         }
         load_to_lds(base, behind, offset, (uint32_t)reinterpret_cast<uintptr_t>((Lds)lds) + place + (wave + 4 * i) * 1024);
     }
@@ -180,6 +191,9 @@ __device__ __forceinline__ void store_out(void *to, bool bf16, size_t at, const 
     else store_eight<float, f32x4>(static_cast<float *>(to) + at, v, n);
 }
 
+// What becomes of eight neighbouring sums, as an End says it: load() brings what it takes besides, finish() computes, put() writes.  Ends that need nothing besides have None.
+struct None {};
+
 // Tiles of 2 x 2 waves, each 32 T rows by 32 T columns of the result.  A step is 64 of k, multiplied in four quarters; the fragments of the
 // next quarter are read while one is multiplied.  Operands are loaded straight into LDS, which has room for five operands' steps: both of the one that is
 // read, both of the next one and the first of the one after that.  So there is always something to load: the second operand of the next step right after the last one's
@@ -194,12 +208,20 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
     // neighbouring blocks go to the eight dies in turn: each die takes a run of tiles, four tile rows high
     const uint32_t total = gridDim.x, die = blockIdx.x & 7u, share = total >> 3, more = total & 7u;
     uint32_t at = die * share + (die < more ? die : more) + (blockIdx.x >> 3);
-    const uint32_t tiles = p.tiles_m * p.tiles_n, whole = uniform(at / tiles), stack = uniform(whole / p.splits), split = whole - stack * p.splits;
+    const uint32_t tiles = p.bands ? half_tiles(p.tiles_m, p.bands) : p.tiles_m * p.tiles_n, whole = uniform(at / tiles), stack = uniform(whole / p.splits), split = whole - stack * p.splits;
     at -= whole * tiles;
-    constexpr uint32_t kHigh = 4;
-    const uint32_t band = uniform(at / (kHigh * p.tiles_n)), in = at - band * kHigh * p.tiles_n;
-    const uint32_t left = p.tiles_m - band * kHigh, high = left < kHigh ? left : kHigh, column = uniform(in / high);
-    const uint32_t m0 = (band * kHigh + in - column * high) * B, n0 = column * B;
+    uint32_t band = 0, first = 0, in;         // first: the band's first column
+    if (p.bands) {
+        while (band + 1 < p.bands && at >= half_tiles(p.tiles_m, band + 1)) ++band;
+        first = band * kHigh;
+        in = at - half_tiles(p.tiles_m, band);
+    } else {
+        band = uniform(at / (kHigh * p.tiles_n));
+        in = at - band * kHigh * p.tiles_n;
+    }
+    const uint32_t left = p.tiles_m - band * kHigh, high = left < kHigh ? left : kHigh, column = first + uniform(in / high);
+    const uint32_t tile_row = band * kHigh + in - (column - first) * high, m0 = tile_row * B, n0 = column * B;
+    if (p.bands && tile_row > column) return;
     const uint32_t each = uniform(p.steps / p.splits), over = p.steps - each * p.splits;
     const uint32_t from = split * each + (split < over ? split : over), to = from + each + (split < over ? 1u : 0u);
 
@@ -207,7 +229,15 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
     const Way<A_DOWN, T> wa(p.a, stack, m0, ma, lane, wave);
     const Way<B_DOWN, T> wb(p.b, stack, n0, nb, lane, wave);
     // the last steps load the last one again, which nothing reads: a branch would part the loop
-    auto step_of = [&](uint32_t step) { return step < to ? step : to - 1; };
+    struct At {
+        uint32_t step;
+        int64_t a, b;
+    };
+    auto step_of = [&](uint32_t step) {
+        step = step < to ? step : to - 1;
+        const bool second = step >= p.once, third = step >= 2 * p.once;
+        return At{third ? step - 2 * p.once : second ? step - p.once : step, second && !third ? p.a.lo * 2 : 0, third ? p.b.lo * 2 : 0};
+    };
     auto read = [&](Fragments<T> &f, int i, int j, uint32_t a, uint32_t b) {
         if (i < T) f.b[i] = wb.read(lds, i, j, b);
         else f.a[i - T] = wa.read(lds, i - T, j, a);
@@ -217,16 +247,18 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
         Fragments<T> f0, f1;
         uint32_t a = 0, b = kUnit, a1 = 2 * kUnit, b1 = 3 * kUnit, free = 4 * kUnit;     // places of this step's operands, the next one's, and of what comes next
 #pragma unroll
-        for (int i = 0; i < L; ++i) wa.fetch(lds, i, a, from, wave), wb.fetch(lds, i, b, from, wave);
+        for (int k = 0; k < 2; ++k) {
+            const At coming = step_of(from + k);
 #pragma unroll
-        for (int i = 0; i < L; ++i) wa.fetch(lds, i, a1, step_of(from + 1), wave), wb.fetch(lds, i, b1, step_of(from + 1), wave);
+            for (int i = 0; i < L; ++i) wa.fetch(lds, i, k ? a1 : a, coming.step, coming.a, wave), wb.fetch(lds, i, k ? b1 : b, coming.step, coming.b, wave);
+        }
         arrived<2 * L>();
         __builtin_amdgcn_s_barrier();
 #pragma unroll
         for (int i = 0; i < 2 * T; ++i) read(f0, i, 0, a, b);
         __builtin_amdgcn_sched_barrier(0);
         for (uint32_t step = from; step < to; ++step) {
-            const uint32_t coming = step_of(step + 2);
+            const At coming = step_of(step + 2);
             // Part by part, with a read and perhaps a load in each: in one go they would keep the matrix unit waiting while their queues are full
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
@@ -237,14 +269,14 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
                 read(f0, part, 2, a, b);
-                if (part % 2 == 0) wa.fetch(lds, part / 2, free, coming, wave);
+                if (part % 2 == 0) wa.fetch(lds, part / 2, free, coming.step, coming.a, wave);
                 multiply<E>(c, f1, part);
                 __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
                 read(f1, part, 3, a, b);
-                if (part % 2 == 0) wa.fetch(lds, T + part / 2, free, coming, wave);
+                if (part % 2 == 0) wa.fetch(lds, T + part / 2, free, coming.step, coming.a, wave);
                 multiply<E>(c, f0, part);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -255,7 +287,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
                 read(f0, part, 0, a1, b1);
-                wb.fetch(lds, part, a, coming, wave);
+                wb.fetch(lds, part, a, coming.step, coming.b, wave);
                 multiply<E>(c, f1, part);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -276,6 +308,13 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
 #pragma unroll
         for (int i = 0; i < T; ++i) {
             char *strip = mine + (i & 1) * kStrip;
+            // all of a strip's loads are on the way together
+            typename End::Besides besides[32 / kRows];
+#pragma unroll
+            for (uint32_t j = 0; j < 32 / kRows; ++j) {
+                const uint32_t m = m0 + ma + i * 32 + j * kRows + of;
+                if (p.splits == 1 && m < p.M && col < p.N) besides[j] = End::load(p.end, stack, m, col, p.N);
+            }
 #pragma unroll
             for (int k = 0; k < T; ++k)
 #pragma unroll
@@ -290,9 +329,30 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
 #pragma unroll
                 for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const f32x4 *>(strip + (row * kChunks + ((2 * eight + h) ^ (row & (kChunks - 1)))) * 16);
                 if (m >= p.M || col >= p.N) continue;
-                if (p.splits == 1) End::store(p.end, stack, m, col, v, p.N);
-                else {
+                if (p.splits > 1) {
                     store_eight<float, f32x4>(p.parts + ((size_t)whole * p.M + m) * p.N + col, v, p.N - col);
+                    continue;
+                }
+                End::finish(p.end, besides[j], m, col, v);
+                End::put(p.end, stack, m, col, v, p.N);
+                if constexpr (End::kSymmetric) {
+                    if (p.bands)       // for the columns, below
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) *reinterpret_cast<f32x4 *>(strip + (row * kChunks + ((2 * eight + h) ^ (row & (kChunks - 1)))) * 16) = v[h];
+                }
+            }
+            if constexpr (End::kSymmetric) {
+                if (!p.bands || tile_row == column) continue;
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                // the same 32 rows as columns: four lanes have a column's eights, one behind the other
+#pragma unroll
+                for (uint32_t j = 0; j < 2 * T; ++j) {
+                    const uint32_t n = j * 16 + (lane >> 2), row = (lane & 3u) * 8;
+                    f32x4 v[2];
+#pragma unroll
+                    for (uint32_t x = 0; x < 8; ++x)
+                        v[x / 4][x % 4] = *reinterpret_cast<const float *>(strip + ((row + x) * kChunks + ((n >> 2) ^ ((row + x) & (kChunks - 1)))) * 16 + (n & 3u) * 4);
+                    if (n0 + nb + n < p.N && m0 + ma + i * 32 + row < p.M) End::put(p.end, stack, n0 + nb + n, m0 + ma + i * 32 + row, v, p.N);
                 }
             }
         }
@@ -328,7 +388,8 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs<typename End::
             for (int x = 0; x < 8; ++x)
                 if (col + x < p.N) v[x / 4][x % 4] += from[k * size + x];
     }
-    End::store(p.end, stack, row, col, v, p.N);
+    End::finish(p.end, End::load(p.end, stack, row, col, p.N), row, col, v);
+    End::put(p.end, stack, row, col, v, p.N);
 }
 
 }  // namespace product
