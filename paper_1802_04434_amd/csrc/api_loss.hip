@@ -86,9 +86,14 @@ struct BackwardPlace {
     }
 };
 
-int copied(const void *from, size_t ld_from, void *to, size_t rows, size_t cols, size_t ld, size_t lines, const int64_t *target, hipStream_t stream) {
-    const loss::CopyArgs a{static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to), target, ld_from, (uint32_t)rows, (uint32_t)cols, (uint32_t)ld, (uint32_t)lines};
-    return launch(loss::copy_kernel, (lines * (ld / 8) + 255) / 256, 0, stream, a, 256);
+loss::Copy copy_of(const void *from, size_t ld_from, void *to, size_t rows, size_t cols, size_t ld, size_t lines, const int64_t *target) {
+    return {static_cast<const uint16_t *>(from), static_cast<uint16_t *>(to), target, ld_from, (uint32_t)rows, (uint32_t)cols, (uint32_t)ld, (uint32_t)lines,
+            (uint32_t)((lines * (ld / 8) + loss::kPrepareThreads - 1) / loss::kPrepareThreads)};
+}
+
+int prepare(const loss::PrepareArgs &a, hipStream_t stream) {
+    const size_t blocks = (a.factors.factor ? 1 : 0) + (size_t)a.h.blocks + a.w.blocks;
+    return blocks ? launch(loss::prepare_kernel, blocks, 0, stream, a, loss::kPrepareThreads) : SS_OK;
 }
 
 int check(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V, size_t K, size_t ldw, const int64_t *target) {
@@ -124,9 +129,9 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
     if (scratch_bytes < ss_cross_entropy_scratch_bytes(T, V, K)) return SS_ERR_ARG;
     char *base = static_cast<char *>(scratch);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+    loss::PrepareArgs before = {};
     if (!loadable(h, K, ldh)) {
-        rc = copied(h, ldh, base + place.h, T, K, s.K64, T, nullptr, stream);
-        if (rc != SS_OK) return rc;
+        before.h = copy_of(h, ldh, base + place.h, T, K, s.K64, T, nullptr);
         h = base + place.h, ldh = s.K64;
     }
     const bool copy = !loadable(w, K, ldw);
@@ -137,11 +142,10 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
     for (size_t v = 0; v < V; v += piece) {
         const size_t n = std::min(piece, V - v);
         const void *from = static_cast<const char *>(w) + v * ldw * 2;
-        if (copy) {
-            rc = copied(from, ldw, base + place.w, n, K, s.K64, n, nullptr, stream);
-            if (rc != SS_OK) return rc;
-            from = base + place.w;
-        }
+        if (copy) before.w = copy_of(from, ldw, base + place.w, n, K, s.K64, n, nullptr), from = base + place.w;
+        rc = prepare(before, stream);
+        if (rc != SS_OK) return rc;
+        before = {};
         const Plan plan = product::plan_of(T, n, s.K64, 1, false);
         const Product p{Operand{h, (uint32_t)ldh, (uint32_t)T, 0, 0, 0}, Operand{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0, 0}, 1, T, n, s.K64 / product::kStep, nullptr};
         rc = product::run<product::Bf16, false, false, loss::StatsEnd>(plan, p, {parts, picked, target, (int64_t)v, (uint32_t)count}, stream);
@@ -179,21 +183,17 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
     float *factor = reinterpret_cast<float *>(base + place.factor), *scale = reinterpret_cast<float *>(base + place.scale);
     float *sum = reinterpret_cast<float *>(base + place.sum), *parts = reinterpret_cast<float *>(base + place.parts);
     __bf16 *d = reinterpret_cast<__bf16 *>(base + place.d);
-    rc = launch(loss::factor_kernel, 1, 0, stream, loss::FactorArgs{dloss, target, factor, scale, (int64_t)V, (uint32_t)T, (uint32_t)s.T64}, 1024);
-    if (rc != SS_OK) return rc;
-    rc = copied(h, ldh, base + place.h, T, K, s.K64, s.T64, target, stream);
-    if (rc != SS_OK) return rc;
+    loss::PrepareArgs before = {{dloss, target, factor, scale, (int64_t)V, (uint32_t)T, (uint32_t)s.T64}, copy_of(h, ldh, base + place.h, T, K, s.K64, s.T64, target), {}};
     const bool copy = !loadable(w, K, ldw);
     const size_t piece = s.backward(copy);
     const uint32_t K64 = (uint32_t)s.K64, T64 = (uint32_t)s.T64;
     for (size_t v = 0; v < V; v += piece) {
         const size_t n = std::min(piece, V - v), n64 = rounded(n, 64);
         const void *from = static_cast<const char *>(w) + v * ldw * 2;
-        if (copy) {
-            rc = copied(from, ldw, base + place.w, n, K, s.K64, n, nullptr, stream);
-            if (rc != SS_OK) return rc;
-            from = base + place.w;
-        }
+        if (copy) before.w = copy_of(from, ldw, base + place.w, n, K, s.K64, n, nullptr), from = base + place.w;
+        rc = prepare(before, stream);
+        if (rc != SS_OK) return rc;
+        before = {};
         const Operand hs{base + place.h, K64, T64, T64, 0, 0}, ws{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0, 0}, ds{d, (uint32_t)n64, T64, 0, 0, 0};
         rc = product::run<product::Bf16, false, false, loss::SoftmaxEnd>(product::plan_of(T64, n64, K64, 1, false), {hs, ws, 1, T64, n64, K64 / product::kStep, nullptr},
                                                                          {lse, factor, target, (int64_t)v, d, (uint32_t)n64, (uint32_t)T, (uint32_t)n}, stream);

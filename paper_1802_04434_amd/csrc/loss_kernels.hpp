@@ -133,15 +133,19 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const JoinArgs a) {
 struct FactorArgs {
     const float *dloss;            // NULL: 1
     const int64_t *target;
-    float *factor, *scale;
+    float *factor, *scale;         // factor NULL: not wanted
     int64_t V;
     uint32_t T, padded;
 };
 
-__global__ __launch_bounds__(1024) void factor_kernel(const FactorArgs a) {
-    __shared__ float tops[16];
+constexpr uint32_t kPrepareThreads = 256;
+
+// by one block
+__device__ __forceinline__ void write_factors(const FactorArgs &a) {
+    __shared__ float tops[kPrepareThreads / 64];
     float top = 0;
-    for (uint32_t t = threadIdx.x; t < a.T; t += 1024) {
+#pragma unroll 4
+    for (uint32_t t = threadIdx.x; t < a.T; t += kPrepareThreads) {
         const float w = a.target[t] < 0 ? 0.0f : a.dloss ? fabsf(a.dloss[t]) : 1.0f;
         top = fmaxf(top, w);       // not of NaN, which its own row's factor keeps
     }
@@ -149,11 +153,12 @@ __global__ __launch_bounds__(1024) void factor_kernel(const FactorArgs a) {
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
     top = 0;
-    for (int k = 0; k < 16; ++k) top = fmaxf(top, tops[k]);
-    // in the range where neither a factor nor a scale loses bits; 1 where there is nothing to weigh
+    for (uint32_t k = 0; k < kPrepareThreads / 64; ++k) top = fmaxf(top, tops[k]);
+    // 1 where there is nothing to weigh, or an infinity
     const float scale = top > 0.0f && top < __builtin_inff() ? top : 1.0f;
     if (threadIdx.x == 0) *a.scale = scale;
-    for (uint32_t t = threadIdx.x; t < a.padded; t += 1024) {
+#pragma unroll 4
+    for (uint32_t t = threadIdx.x; t < a.padded; t += kPrepareThreads) {
         float f = 0;
         if (t < a.T) {
             const int64_t target = a.target[t];
@@ -240,16 +245,17 @@ struct GradientEnd {
 
 // rows x cols elements with zeros around them, rows of `ld` (a multiple of 64) elements from 16-byte aligned memory: an operand that the products can load.
 // Rows without a target become zero, so that whatever a padded batch holds there meets a zero of D as a zero.
-struct CopyArgs {
+struct Copy {
     const uint16_t *from;
     uint16_t *to;
     const int64_t *target;         // NULL: all rows stay
     uint64_t ld_from;
     uint32_t rows, cols, ld, lines;
+    uint32_t blocks;               // 0: nothing to copy
 };
 
-__global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a) {
-    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
+__device__ __forceinline__ void copy_rows(const Copy &a, uint32_t block) {
+    const uint64_t at = (uint64_t)block * kPrepareThreads + threadIdx.x;
     const uint32_t across = a.ld / 8;
     const uint32_t row = (uint32_t)(at / across), col = (uint32_t)(at - (uint64_t)row * across) * 8;
     if (row >= a.lines) return;
@@ -263,6 +269,19 @@ __global__ __launch_bounds__(256) void copy_kernel(const CopyArgs a) {
                 if (col + x < a.cols) v[x / 2] |= (uint32_t)from[x] << (x % 2 * 16);
     }
     *reinterpret_cast<u32x4 *>(a.to + (size_t)row * a.ld + col) = v;
+}
+
+// What comes before the products, in one launch: the rows' factors by the first block, then the copies.
+struct PrepareArgs {
+    FactorArgs factors;
+    Copy h, w;
+};
+
+__global__ __launch_bounds__(kPrepareThreads) void prepare_kernel(const PrepareArgs a) {
+    uint32_t block = blockIdx.x;
+    if (a.factors.factor && block-- == 0) write_factors(a.factors);
+    else if (block < a.h.blocks) copy_rows(a.h, block);
+    else copy_rows(a.w, block - a.h.blocks);
 }
 
 // the gradient of no rows at all

@@ -364,14 +364,16 @@ struct JoinArgs {
     const float *parts;
     uint32_t M, N, splits, across;      // across: eights of a row
     uint64_t eights;                    // of all rows of the stack
+    uint32_t slices;                    // threads that share an eight's parts: a power of two, 64 at most
     EndArgs end;
 };
 
-// the partial sums, one after the other, eight neighbours a lane
+// The partial sums, eight neighbours a lane; where there are few of them and many parts, several lanes share them: 2 x 212 in 256 parts JOIN_FEW us (one lane for each 23).
 template <typename End>
 __global__ __launch_bounds__(256) void join_kernel(const JoinArgs<typename End::Args> p) {
-    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x;
-    if (at >= p.eights) return;
+    const uint64_t thread = (uint64_t)blockIdx.x * 256 + threadIdx.x, at = thread / p.slices;
+    const uint32_t slice = (uint32_t)thread & (p.slices - 1);
+    if (at >= p.eights) return;         // whole groups of slices
     const uint64_t line = at / p.across;
     const uint32_t col = (uint32_t)(at - line * p.across) * 8, stack = (uint32_t)(line / p.M), row = (uint32_t)(line - (uint64_t)stack * p.M);
     const size_t size = (size_t)p.M * p.N;
@@ -379,15 +381,19 @@ __global__ __launch_bounds__(256) void join_kernel(const JoinArgs<typename End::
     f32x4 v[2] = {};
     if (col + 8 <= p.N) {
 #pragma unroll 4
-        for (uint32_t k = 0; k < p.splits; ++k)
+        for (uint32_t k = slice; k < p.splits; k += p.slices)
 #pragma unroll
             for (int h = 0; h < 2; ++h) v[h] += *reinterpret_cast<const f32x4_any *>(from + k * size + 4 * h);
     } else {
-        for (uint32_t k = 0; k < p.splits; ++k)
+        for (uint32_t k = slice; k < p.splits; k += p.slices)
 #pragma unroll
             for (int x = 0; x < 8; ++x)
                 if (col + x < p.N) v[x / 4][x % 4] += from[k * size + x];
     }
+    for (uint32_t apart = 1; apart < p.slices; apart *= 2)
+#pragma unroll
+        for (int x = 0; x < 8; ++x) v[x / 4][x % 4] += __shfl_xor(v[x / 4][x % 4], apart);
+    if (slice) return;
     End::finish(p.end, End::load(p.end, stack, row, col, p.N), row, col, v);
     End::put(p.end, stack, row, col, v, p.N);
 }

@@ -75,9 +75,12 @@ int run(const Plan &plan, const Product &p, const typename End::Args &end, hipSt
     if (rc != SS_OK || plan.splits == 1) return rc;
     if constexpr (End::kStrips) {
         const uint64_t across = (p.N + 7) / 8, eights = across * p.M * p.count;
-        if ((eights + 255) / 256 > kMaxBlocks) return SS_ERR_ARG;
-        const JoinArgs<typename End::Args> join{p.parts, (uint32_t)p.M, (uint32_t)p.N, (uint32_t)plan.splits, (uint32_t)across, eights, end};
-        return host::launch(join_kernel<End>, (eights + 255) / 256, 0, stream, join, 256);
+        uint32_t slices = 1;      // until there is a block for each compute unit, or two parts for a lane
+        while (slices < 64 && eights * slices < 256 * 256 && 4 * slices <= plan.splits) slices *= 2;
+        const uint64_t blocks_of = (eights * slices + 255) / 256;
+        if (blocks_of > kMaxBlocks) return SS_ERR_ARG;
+        const JoinArgs<typename End::Args> join{p.parts, (uint32_t)p.M, (uint32_t)p.N, (uint32_t)plan.splits, (uint32_t)across, eights, slices, end};
+        return host::launch(join_kernel<End>, blocks_of, 0, stream, join, 256);
     }
     return SS_ERR_ARG;
 }
