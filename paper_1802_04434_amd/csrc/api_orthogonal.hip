@@ -60,10 +60,10 @@ struct Place {
         for (Plans *p : {&once, &twofold}) {
             const size_t times = p == &twofold ? 3 : 1;
             p->square = product::plan_of(shorter, shorter, times * longer, s.count, true, true);
-            p->polynomial = product::plan_of(shorter, shorter, times * shorter, s.count, true, true);
-            p->update = product::plan_of(rows, cols, times * shorter, s.count, true);
+            p->polynomial = product::plan_of(shorter, shorter, times * shorter, s.count, false, true);
+            p->update = product::plan_of(rows, cols, times * shorter, s.count, false);
             if (p == &once || some)
-                most = std::max({most, parts_bytes(p->square, s.count, shorter, shorter), parts_bytes(p->polynomial, s.count, shorter, shorter), parts_bytes(p->update, s.count, rows, cols)});
+                most = std::max(most, parts_bytes(p->square, s.count, shorter, shorter));
         }
         parts = l.take(most);
         bytes = l.bytes;

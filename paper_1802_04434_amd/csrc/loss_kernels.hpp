@@ -25,7 +25,7 @@ struct Part {
 };
 
 struct StatsEnd {
-    static constexpr bool kStrips = false;
+    static constexpr bool kStrips = false, kParts = false;
     struct Args {
         Part *parts;               // (half a tile's columns, row)
         float *picked;             // the target's logit, by row
@@ -170,7 +170,7 @@ __device__ __forceinline__ void write_factors(const FactorArgs &a) {
 
 // D, whole eights of columns and rows: zero beyond the vocabulary and in rows without a target
 struct SoftmaxEnd {
-    static constexpr bool kStrips = true, kSymmetric = false;
+    static constexpr bool kStrips = true, kParts = false, kSymmetric = false;
     struct Args {
         const float *lse, *factor;
         const int64_t *target;
@@ -203,7 +203,7 @@ struct SoftmaxEnd {
 
 // A gradient, or with the pieces before it the sum so far
 struct GradientEnd {
-    static constexpr bool kStrips = true, kSymmetric = false;
+    static constexpr bool kStrips = true, kParts = true, kSymmetric = false;
     struct Args {
         const float *scale;
         float *sum;                // rows x N: not wanted where a piece is all there is

@@ -191,7 +191,8 @@ __device__ __forceinline__ void store_out(void *to, bool bf16, size_t at, const 
     else store_eight<float, f32x4>(static_cast<float *>(to) + at, v, n);
 }
 
-// What becomes of eight neighbouring sums, as an End says it: load() brings what it takes besides, finish() computes, put() writes.  Ends that need nothing besides have None.
+// What becomes of eight neighbouring sums, as an End says it: load() brings what it takes besides (None where that is nothing), finish() computes, put() writes.  kStrips: it is given
+// them so, and not a wave's whole tile; kParts: the sum over k may come in parts; kSymmetric: the result may be computed by half.
 struct None {};
 
 // Tiles of 2 x 2 waves, each 32 T rows by 32 T columns of the result.  A step is 64 of k, multiplied in four quarters; the fragments of the
@@ -313,7 +314,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
 #pragma unroll
             for (uint32_t j = 0; j < 32 / kRows; ++j) {
                 const uint32_t m = m0 + ma + i * 32 + j * kRows + of;
-                if (p.splits == 1 && m < p.M && col < p.N) besides[j] = End::load(p.end, stack, m, col, p.N);
+                if ((!End::kParts || p.splits == 1) && m < p.M && col < p.N) besides[j] = End::load(p.end, stack, m, col, p.N);
             }
 #pragma unroll
             for (int k = 0; k < T; ++k)
@@ -329,9 +330,11 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
 #pragma unroll
                 for (int h = 0; h < 2; ++h) v[h] = *reinterpret_cast<const f32x4 *>(strip + (row * kChunks + ((2 * eight + h) ^ (row & (kChunks - 1)))) * 16);
                 if (m >= p.M || col >= p.N) continue;
-                if (p.splits > 1) {
-                    store_eight<float, f32x4>(p.parts + ((size_t)whole * p.M + m) * p.N + col, v, p.N - col);
-                    continue;
+                if constexpr (End::kParts) {
+                    if (p.splits > 1) {
+                        store_eight<float, f32x4>(p.parts + ((size_t)whole * p.M + m) * p.N + col, v, p.N - col);
+                        continue;
+                    }
                 }
                 End::finish(p.end, besides[j], m, col, v);
                 End::put(p.end, stack, m, col, v, p.N);

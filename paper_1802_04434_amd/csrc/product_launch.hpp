@@ -73,7 +73,7 @@ int run(const Plan &plan, const Product &p, const typename End::Args &end, hipSt
     const auto kernel = plan.tile == 4 ? tiles_kernel<E, A_DOWN, B_DOWN, 4, End> : plan.tile == 2 ? tiles_kernel<E, A_DOWN, B_DOWN, 2, End> : tiles_kernel<E, A_DOWN, B_DOWN, 1, End>;
     const int rc = host::launch(kernel, blocks, 0, stream, args, 256);
     if (rc != SS_OK || plan.splits == 1) return rc;
-    if constexpr (End::kStrips) {
+    if constexpr (End::kParts) {
         const uint64_t across = (p.N + 7) / 8, eights = across * p.M * p.count;
         uint32_t slices = 1;      // until there is a block for each compute unit, or two parts for a lane
         while (slices < 64 && eights * slices < 256 * 256 && 4 * slices <= plan.splits) slices *= 2;

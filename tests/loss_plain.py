@@ -1,5 +1,7 @@
 """The loss over a vocabulary and orthogonalised updates from their definitions in 64 bits, with the bounds that the kernels'
 roundings have: operands of products rounded to 16 bits by at most half a step, sums in fp32."""
+import math
+
 import torch
 
 U32, U16, H16 = 2.0 ** -24, 2.0 ** -8, 2.0 ** -11       # half a step of fp32, bf16 and fp16, relative
@@ -21,12 +23,12 @@ def softmax_loss(h, w, target, dloss=None):
     ez = 2 * U32 * K * (h64.abs() @ w64.abs().t())
     # exp(z - top): the difference and its product with log2(e) are rounded, so is the function; the terms' errors weigh as their share p, and
     # the sum of p |log p| is at most log V; 32 T terms of a lane, then the parts
-    log_v = torch.log(torch.tensor(float(V), dtype=torch.float64))
+    log_v = math.log(V)
     e_lse = ez.amax(1) + 2 * U32 * (2 * log_v + 8 + 80 + V / 32) + 2 * U32 * lse.abs()
     e_loss = torch.where(there, e_lse + ez.gather(1, target.clamp(0, V - 1)[:, None])[:, 0] + U32 * (lse - picked).abs(), 0.0)
     p = (z - lse[:, None]).exp()
     d = p.clone()
-    d[torch.arange(len(d)), target.clamp(0, V - 1)] -= 1.0
+    d[torch.arange(len(d), device=d.device), target.clamp(0, V - 1)] -= 1.0
     d *= weight[:, None]
     ep = p * (ez + e_lse[:, None] + 4 * U32 * ((z - lse[:, None]).abs() + 4))
     ed = ep * weight.abs()[:, None] + (U16 + 8 * U32) * d.abs()
@@ -57,12 +59,12 @@ def rounded_steps(g, steps, gen):
     tall = x.shape[0] > x.shape[1]
     x = x.t() if tall else x
     x = x / x.norm()
-    off = lambda t, h: t * (1 + h * (2 * torch.rand(t.shape, generator=gen, dtype=torch.float64) - 1))  # noqa: E731
+    off = lambda t, h: t * (1 + h * (2 * torch.rand(t.shape, generator=gen, dtype=torch.float64, device=t.device) - 1))  # noqa: E731
     for k in range(steps):
         mu = {1: 2.0, 2: 0.8}.get(steps - k, 0.0)
         hi = off(x, H16)
         p = off(hi @ hi.t(), H16)
-        b = off(B * p + C * p @ p + mu * torch.eye(len(p), dtype=torch.float64), H16)
+        b = off(B * p + C * p @ p + mu * torch.eye(len(p), dtype=torch.float64, device=p.device), H16)
         x = off((A - mu) * x + b @ hi, H16 ** 2)
     return x.t() if tall else x
 
@@ -74,6 +76,6 @@ def orthogonal_bound(g, steps=5):
     15 roundings of an entry, of equal weight, are off by (3 x 15)^1/2 = 6.7 deviations at most, a draw of eight by one at least.  Sums in fp32 over
     k terms are off by k^1/2 2^-24, a hundredth of that."""
     want = orthogonalized(g, steps)
-    gen = torch.Generator().manual_seed(g.shape[0] * 8191 + g.shape[1])
+    gen = torch.Generator(device=g.device).manual_seed(g.shape[0] * 8191 + g.shape[1])
     few = g.numel() < 256
     return (6 if few else 3) * max(float((rounded_steps(g, steps, gen) - want).norm()) for _ in range(8 if few else 4))

@@ -13,6 +13,9 @@ NAN = float("nan")
 SIZES = [(1, 1, 1), (1, 2, 64), (1, 1000, 8), (2, 63, 7), (3, 64, 64), (5, 65, 63), (31, 255, 65), (33, 257, 128), (63, 127, 96), (64, 128, 64),
          (65, 129, 72), (100, 33, 200), (127, 513, 130), (128, 1000, 256), (129, 2049, 40), (257, 300, 520), (300, 700, 192), (513, 96, 320)]
 
+# every tile size, several pieces of the vocabulary (also of copied weights), sums in parts; compared with 64 bits on the GPU
+LARGE = [(1, 70_001, 64), (2, 30_000, 200), (40, 257, 8192), (1500, 4100, 256), (2600, 5000, 320), (5000, 9000, 1000), (33_000, 2200, 72), (3, 1500, 60_001)]
+
 
 def sliced(x, pad, offset):
     """x as a slice of a buffer of NaN: rows `pad` further apart than they are long, the first `offset` elements in"""
@@ -49,7 +52,7 @@ def both(h, w, target, dloss, scratch, dh_type=torch.bfloat16, dw_type=torch.bfl
 
 def check(got, want, rows=None):
     for name, (value, bound) in want.items():
-        g = got[name].cpu()
+        g, value, bound = got[name].cpu(), value.cpu(), bound.cpu()
         half = {torch.float32: plain.U32, torch.bfloat16: plain.U16}[g.dtype]
         bound = bound + 2 * half * value.abs() + 1e-30
         off = (g.double() - value).abs()
@@ -71,6 +74,19 @@ def test_loss_and_gradients(T, V, K):
             t = got[name]
             around = t.as_strided((t.shape[0] - 1, pad), (t.stride(0), 1), t.storage_offset() + t.shape[1]) if pad and t.shape[0] > 1 else None
             assert around is None or torch.isnan(around).all(), name
+
+
+@pytest.mark.parametrize("T,V,K", LARGE)
+def test_large_sizes(T, V, K):
+    gen = torch.Generator(device=DEV).manual_seed(T + V + K)
+    h = torch.randn(T, K, generator=gen, device=DEV).bfloat16()
+    w = (torch.randn(V, K, generator=gen, device=DEV) * 2 / K ** 0.5).bfloat16()
+    target = torch.randint(0, V, (T,), generator=gen, device=DEV)
+    target[torch.rand(T, generator=gen, device=DEV) < 0.2] = -1
+    target[0] = V - 1
+    dloss = torch.randn(T, generator=gen, device=DEV)
+    got = both(h, w, target, dloss, scratch_for(T, V, K))
+    check(got, plain.softmax_loss(h, w, target, dloss), (target >= 0).cpu())
 
 
 @pytest.mark.parametrize("dh_type", [torch.float32, torch.bfloat16])

@@ -11,7 +11,10 @@ DEV = "cuda"
 NAN = float("nan")
 DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 # one entry to several tiles, wide, tall and square, both sides of 8, 64, 128 and 256
-SHAPES = [(1, 1), (1, 7), (9, 1), (1, 500), (3, 5), (8, 64), (63, 65), (64, 64), (65, 33), (100, 300), (129, 128), (257, 40), (200, 257), (260, 260), (96, 1100), (700, 130)]
+SHAPES = [(1, 1), (1, 7), (9, 1), (1, 500), (3, 5), (8, 64), (63, 65), (64, 64), (65, 33), (70, 90), (100, 300), (129, 128), (257, 40), (200, 257), (260, 260), (96, 1100), (700, 130)]
+
+# each number of steps in 22 bits, halves of symmetric products of every tile size, sums in parts
+LARGE = [(300, 700), (600, 520), (530, 2000), (2050, 1030), (140, 5000), (5000, 300), (2100, 2200), (3000, 3100)]
 
 
 def matrix(rows, cols, seed=0, kind="gradient"):
@@ -62,6 +65,23 @@ def test_orthogonalize(rows, cols, dtype):
         buffer = out.as_strided((out.untyped_storage().nbytes() // out.element_size(),), (1,), 0).clone()
         buffer.as_strided(out.shape, out.stride(), offset).fill_(NAN)
         assert torch.isnan(buffer).all()                 # around the matrices nothing is written
+
+
+@pytest.mark.parametrize("rows,cols", LARGE)
+def test_large_matrices(rows, cols):
+    """both types of result, and the whole step, against 64 bits on the GPU; the bound of a matrix with the same spectrum and fewer entries would be larger"""
+    x = matrix(rows, cols, 3).to(DEV)
+    want, bound = plain.orthogonalized(x), plain.orthogonal_bound(x)
+    scratch = scratch_for(rows, cols)
+    for odt, half in ((torch.bfloat16, plain.U16), (torch.float32, plain.U32)):
+        out = torch.empty(rows, cols, dtype=odt, device=DEV)
+        ss.orthogonalize(x, out, scratch)
+        off = float((out.double() - want).norm())
+        assert off <= bound + half * float(want.norm()), (odt, off, bound)
+    m, p = torch.zeros_like(x), torch.ones_like(x)
+    ss.orthogonal_step(x, m, 0.5, 1.0, p, scratch)
+    off = float((p.double() - (1.0 - want)).norm())
+    assert off <= bound + 3 * plain.U32 * float(want.norm() + p.numel() ** 0.5), (off, bound)
 
 
 @pytest.mark.parametrize("kind", ["normal", "singular"])
