@@ -464,8 +464,8 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
  *                 has run (two calls that may run at the same time, or two captured graphs that may,
  *                 need two).  Smaller: SS_ERR_ARG.
  * T may be 0; V and K may not, and none may exceed the limits below (SS_ERR_ARG).  Nothing that is written
- * may share a byte with anything else of the call.  Rows whose K is a multiple of 64, whose ld is one of 8 and
- * that are 16-byte aligned are read where they are; others are copied into scratch on the way, piece by piece.
+ * may share a byte with anything else of the call.  w is read where it is if its rows are 16-byte aligned (4-byte
+ * where T is small), else copied into scratch on the way, piece by piece.
  * Sums are added in an order that depends on the sizes and on that alone.
  */
 #define SS_LOSS_MAX_ROWS ((size_t)1 << 24)

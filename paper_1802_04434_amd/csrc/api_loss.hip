@@ -24,8 +24,27 @@ inline Span matrix(const void *p, size_t rows, size_t cols, size_t ld, ss_dtype 
 inline bool bad_sizes(size_t T, size_t V, size_t K) { return T > SS_LOSS_MAX_ROWS || V > SS_LOSS_MAX_VOCAB || K == 0 || K > SS_LOSS_MAX_WIDTH || V == 0; }
 inline bool bad_ld(size_t ld, size_t cols) { return ld < cols || ld > 2 * SS_LOSS_MAX_WIDTH; }
 
-// whether the products can load a matrix as it lies: whole steps of k, rows at multiples of 16 bytes
-inline bool loadable(const void *p, size_t K, size_t ld) { return K % product::kStep == 0 && ld % 8 == 0 && aligned16(p); }
+// Whether the products load the caller's matrix as it lies.  Rows at multiples of 16 bytes are; a load of 16 bytes also goes to multiples of 4, but takes longer, which many rows of h
+// repeat and a copy does not.  us, w as it lies / copied: a training pass of 2 rows against 19840 x 2258 134 / 171, of 1284 against 3350 x 1118 120 / 115.
+inline bool loadable(const void *p, size_t ld, size_t T) {
+    if (ld % 8 == 0 && aligned16(p)) return true;
+    return T < 1024 && ld % 2 == 0 && reinterpret_cast<uintptr_t>(p) % 4 == 0;
+}
+inline bool whole(size_t K) { return K % product::kStep == 0; }
+
+// a caller's rows as an operand
+inline Operand rows_of(const void *p, size_t rows, size_t cols, size_t ld, size_t m, size_t depth) {
+    return {p, (uint32_t)ld, (uint32_t)m, (uint32_t)depth, 0, 0, rounded(((rows - 1) * ld + cols) * 2, 4)};
+}
+
+// a product with the weights along their columns
+template <template <bool> class End>
+int along_weights(const Plan &plan, Product p, size_t K, bool copy, const typename End<false>::Args &end, hipStream_t stream) {
+    p.tail = copy || whole(K) ? product::kStep : K % product::kStep;
+    if (p.tail == product::kStep) return product::run<product::Bf16, false, false, End<false>>(plan, p, end, stream);
+    static_assert(sizeof(typename End<true>::Args) == sizeof end, "the same fields");
+    return product::run<product::Bf16, false, false, End<true>>(plan, p, __builtin_bit_cast(typename End<true>::Args, end), stream);
+}
 
 // What is computed at a time is a piece of the vocabulary.  Forward: 2^36 entries of z, or 128 MB of copied weights.  Backward: 128 MB of D, so that
 // the products that read it find it in the memory-side cache.
@@ -130,11 +149,11 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
     char *base = static_cast<char *>(scratch);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
     loss::PrepareArgs before = {};
-    if (!loadable(h, K, ldh)) {
+    if (!loadable(h, ldh, T) || !whole(K)) {
         before.h = copy_of(h, ldh, base + place.h, T, K, s.K64, T, nullptr);
         h = base + place.h, ldh = s.K64;
     }
-    const bool copy = !loadable(w, K, ldw);
+    const bool copy = !loadable(w, ldw, T);
     const size_t piece = s.forward(copy);
     loss::Part *parts = reinterpret_cast<loss::Part *>(base + place.parts);
     float *picked = reinterpret_cast<float *>(base + place.picked);
@@ -147,8 +166,9 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
         if (rc != SS_OK) return rc;
         before = {};
         const Plan plan = product::plan_of(T, n, s.K64, 1, false);
-        const Product p{Operand{h, (uint32_t)ldh, (uint32_t)T, 0, 0, 0}, Operand{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0, 0}, 1, T, n, s.K64 / product::kStep, nullptr};
-        rc = product::run<product::Bf16, false, false, loss::StatsEnd>(plan, p, {parts, picked, target, (int64_t)v, (uint32_t)count}, stream);
+        const Operand ws = copy ? rows_of(from, n, s.K64, s.K64, n, 0) : rows_of(from, n, K, ldw, n, 0);
+        rc = along_weights<loss::StatsEnd>(plan, {rows_of(h, T, s.K64, ldh, T, 0), ws, 1, T, n, s.K64 / product::kStep, nullptr}, K, copy,
+                                           {parts, picked, target, (int64_t)v, (uint32_t)count}, stream);
         if (rc != SS_OK) return rc;
         count += 2 * tiles_of(n, plan.tile);
     }
@@ -184,7 +204,7 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
     float *sum = reinterpret_cast<float *>(base + place.sum), *parts = reinterpret_cast<float *>(base + place.parts);
     __bf16 *d = reinterpret_cast<__bf16 *>(base + place.d);
     loss::PrepareArgs before = {{dloss, target, factor, scale, (int64_t)V, (uint32_t)T, (uint32_t)s.T64}, copy_of(h, ldh, base + place.h, T, K, s.K64, s.T64, target), {}};
-    const bool copy = !loadable(w, K, ldw);
+    const bool copy = !loadable(w, ldw, T);
     const size_t piece = s.backward(copy);
     const uint32_t K64 = (uint32_t)s.K64, T64 = (uint32_t)s.T64;
     for (size_t v = 0; v < V; v += piece) {
@@ -194,19 +214,19 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
         rc = prepare(before, stream);
         if (rc != SS_OK) return rc;
         before = {};
-        const Operand hs{base + place.h, K64, T64, T64, 0, 0}, ws{from, (uint32_t)(copy ? s.K64 : ldw), (uint32_t)n, 0, 0, 0}, ds{d, (uint32_t)n64, T64, 0, 0, 0};
-        rc = product::run<product::Bf16, false, false, loss::SoftmaxEnd>(product::plan_of(T64, n64, K64, 1, false), {hs, ws, 1, T64, n64, K64 / product::kStep, nullptr},
-                                                                         {lse, factor, target, (int64_t)v, d, (uint32_t)n64, (uint32_t)T, (uint32_t)n}, stream);
+        const Operand hs{base + place.h, K64, T64, T64, 0, 0, 0}, ds{d, (uint32_t)n64, T64, 0, 0, 0, 0}, ws = copy ? rows_of(from, n, s.K64, s.K64, n, 0) : rows_of(from, n, K, ldw, n, 0);
+        rc = along_weights<loss::SoftmaxEnd>(product::plan_of(T64, n64, K64, 1, false), {hs, ws, 1, T64, n64, K64 / product::kStep, nullptr}, K, copy,
+                                             {lse, factor, target, (int64_t)v, d, (uint32_t)n64, (uint32_t)T, (uint32_t)n}, stream);
         if (rc != SS_OK) return rc;
         if (dh) {
             // the weights lie down their tokens
-            const Operand down{from, ws.ld, (uint32_t)K, (uint32_t)n, 0, 0};
+            const Operand down = copy ? rows_of(from, n, s.K64, s.K64, K, n) : rows_of(from, n, K, ldw, K, n);
             rc = product::run<product::Bf16, false, true, loss::GradientEnd>(product::plan_of(T, K, n64, 1, true), {ds, down, 1, T, K, n64 / product::kStep, parts},
                                                                              {scale, sum, dh, lddh, v == 0, v + piece >= V, dhdt == SS_BF16}, stream);
             if (rc != SS_OK) return rc;
         }
         if (dw) {
-            const Operand d_down{d, (uint32_t)n64, (uint32_t)n64, T64, 0, 0}, h_down{base + place.h, K64, (uint32_t)K, T64, 0, 0};
+            const Operand d_down{d, (uint32_t)n64, (uint32_t)n64, T64, 0, 0, 0}, h_down{base + place.h, K64, (uint32_t)K, T64, 0, 0, 0};
             rc = product::run<product::Bf16, true, true, loss::GradientEnd>(
                 product::plan_of(n, K, s.T64, 1, true), {d_down, h_down, 1, n, K, s.T64 / product::kStep, parts},
                 {scale, nullptr, static_cast<char *>(dw) + v * lddw * grad_bytes(dwdt), lddw, true, true, dwdt == SS_BF16}, stream);

@@ -132,7 +132,7 @@ int orthogonalized(const Stack &s, const Ends &e, int steps, char *scratch, hipS
         const float mu = last ? kLast : k + 2 == steps ? kBefore : 0.0f;
         const int at = k & 1, next = ~k & 1;
         const Plans &plans = twofold ? place.twofold : place.once;
-        const Operand x{hi[at], C, R, R, whole, lo[at] - hi[at]}, down{hi[at], C, C, R, whole, lo[at] - hi[at]}, as{a[0], S, S, S, square, a[1] - a[0]}, bs{b[0], S, S, S, square, b[1] - b[0]};
+        const Operand x{hi[at], C, R, R, whole, lo[at] - hi[at], 0}, down{hi[at], C, C, R, whole, lo[at] - hi[at], 0}, as{a[0], S, S, S, square, a[1] - a[0], 0}, bs{b[0], S, S, S, square, b[1] - b[0], 0};
         _Float16 *const a_lo = twofold ? a[1] : nullptr, *const b_lo = twofold ? b[1] : nullptr;
         const SquareEnd::Args square_end{a[0], a_lo, square};
         if (tall) rc = product::run<product::F16, true, true, SquareEnd>(plans.square, {down, down, s.count, S, S, R / product::kStep, parts, twofold}, square_end, stream);

@@ -24,8 +24,9 @@ struct Part {
     float top, sum;
 };
 
+template <bool RAGGED>
 struct StatsEnd {
-    static constexpr bool kStrips = false, kParts = false;
+    static constexpr bool kStrips = false, kParts = false, kRagged = RAGGED;
     struct Args {
         Part *parts;               // (half a tile's columns, row)
         float *picked;             // the target's logit, by row
@@ -144,11 +145,23 @@ constexpr uint32_t kPrepareThreads = 256;
 __device__ __forceinline__ void write_factors(const FactorArgs &a) {
     __shared__ float tops[kPrepareThreads / 64];
     float top = 0;
-#pragma unroll 4
-    for (uint32_t t = threadIdx.x; t < a.T; t += kPrepareThreads) {
-        const float w = a.target[t] < 0 ? 0.0f : a.dloss ? fabsf(a.dloss[t]) : 1.0f;
-        top = fmaxf(top, w);       // not of NaN, which its own row's factor keeps
-    }
+    // eight rows' loads on the way together
+    auto rows = [&](uint32_t count, auto each) {
+        for (uint32_t t0 = threadIdx.x; t0 < count; t0 += 8 * kPrepareThreads) {
+            int64_t target[8];
+            float w[8];
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x) {
+                const uint32_t t = t0 + x * kPrepareThreads;
+                target[x] = t < a.T ? a.target[t] : -1;
+                w[x] = t < a.T && a.dloss ? a.dloss[t] : 1.0f;
+            }
+#pragma unroll
+            for (uint32_t x = 0; x < 8; ++x)
+                if (t0 + x * kPrepareThreads < count) each(t0 + x * kPrepareThreads, target[x], w[x]);
+        }
+    };
+    rows(a.T, [&](uint32_t, int64_t target, float w) { top = fmaxf(top, target < 0 ? 0.0f : fabsf(w)); });      // not of NaN, which its own row's factor keeps
     for (int x = 32; x; x >>= 1) top = fmaxf(top, __shfl_xor(top, x));
     if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
     __syncthreads();
@@ -157,20 +170,13 @@ __device__ __forceinline__ void write_factors(const FactorArgs &a) {
     // 1 where there is nothing to weigh, or an infinity
     const float scale = top > 0.0f && top < __builtin_inff() ? top : 1.0f;
     if (threadIdx.x == 0) *a.scale = scale;
-#pragma unroll 4
-    for (uint32_t t = threadIdx.x; t < a.padded; t += kPrepareThreads) {
-        float f = 0;
-        if (t < a.T) {
-            const int64_t target = a.target[t];
-            f = target < 0 ? 0.0f : target >= a.V ? __builtin_nanf("") : (a.dloss ? a.dloss[t] : 1.0f) / scale;
-        }
-        a.factor[t] = f;
-    }
+    rows(a.padded, [&](uint32_t t, int64_t target, float w) { a.factor[t] = target < 0 ? 0.0f : target >= a.V ? __builtin_nanf("") : w / scale; });
 }
 
 // D, whole eights of columns and rows: zero beyond the vocabulary and in rows without a target
+template <bool RAGGED>
 struct SoftmaxEnd {
-    static constexpr bool kStrips = true, kParts = false, kSymmetric = false;
+    static constexpr bool kStrips = true, kParts = false, kSymmetric = false, kRagged = RAGGED;
     struct Args {
         const float *lse, *factor;
         const int64_t *target;
@@ -203,7 +209,7 @@ struct SoftmaxEnd {
 
 // A gradient, or with the pieces before it the sum so far
 struct GradientEnd {
-    static constexpr bool kStrips = true, kParts = true, kSymmetric = false;
+    static constexpr bool kStrips = true, kParts = true, kSymmetric = false, kRagged = false;
     struct Args {
         const float *scale;
         float *sum;                // rows x N: not wanted where a piece is all there is

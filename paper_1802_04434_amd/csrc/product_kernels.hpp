@@ -43,11 +43,12 @@ constexpr uint32_t kStep = 64;      // k of one step
 
 struct Operand {
     const void *p;
-    uint32_t ld;         // elements from one row to the next; rows start at multiples of 16 bytes
+    uint32_t ld;         // elements from one row to the next; rows start at multiples of 4 bytes
     uint32_t rows;       // m there are: those beyond read as the last one, or what lies behind it in its 16 bytes
-    uint32_t depth;      // k there are, of an operand that lies down: those beyond read as the last one.  Along k there are whole steps.
+    uint32_t depth;      // k there are, of an operand that lies down: those beyond read as the last one.  Along k there are whole steps, or what stands in their place is masked (kRagged).
     uint64_t apart;      // elements from one matrix of a stack to the next
     int64_t lo;          // of an operand that is the sum of two: elements from one to the other
+    uint64_t bytes;      // a caller's buffer: what lies beyond is not read, and zero.  0: memory of our own, which goes on
 };
 
 constexpr uint32_t kHigh = 4;      // tile rows of a band, in which tiles are taken column by column
@@ -63,6 +64,7 @@ struct TilesArgs {
     Operand a, b;
     uint32_t M, N;                    // of the result
     uint32_t steps;
+    uint32_t tail;                    // k of the last step, if it is ragged
     uint32_t once;                    // steps of one product.  Operands that are sums of two take three: first times first, A's second times first, first times B's second.
     uint32_t tiles_m, tiles_n;
     uint32_t splits;                  // of k
@@ -76,12 +78,13 @@ template <int N>
 __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
 
 // 16 bytes a lane straight into LDS, one lane's behind the other's from `to` on.  Not by the builtin: after one the compiler lets no ds_read_b64_tr_b16 go before all loads into LDS are there, whatever
-// part of it they go to (8192 x 4096 x 8192 with both operands down k 1,191 us).  What a step reads has been waited for with arrived().
+// part of it they go to (8192 x 4096 x 8192 with both operands down k 1,191 us).  What a step reads has been waited for with arrived().  Addresses are multiples of 4 bytes; a dword beyond `end`
+// is not read, and zero in LDS.
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"      // m0 is reserved, but not in use here: no other instruction of these kernels reads it
-__device__ __forceinline__ void load_to_lds(const char *base, size_t behind, uint32_t offset, uint32_t to) {
-    const uint64_t p = reinterpret_cast<uint64_t>(base) + behind;
-    const u32x4 window = {(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, 0xFFFFFFFFu, 0x00020000u};
+__device__ __forceinline__ void load_to_lds(const char *base, size_t behind, uint64_t end, uint32_t offset, uint32_t to) {
+    const uint64_t p = reinterpret_cast<uint64_t>(base) + behind, left = end > p ? end - p : 0;
+    const u32x4 window = {(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, left < 0xFFFFFFFFu ? (uint32_t)left : 0xFFFFFFFFu, 0x00020000u};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(offset), "s"(window) : "m0");
 }
 #pragma clang diagnostic pop
@@ -99,13 +102,15 @@ struct Way {
     static constexpr uint32_t kRow = DOWN ? 128 * T : 128, kPerLoad = 1024 / kRow;
     static constexpr int kLoads = 2 * T;     // of a wave, for a step
     const char *base;
+    uint64_t end;
     uint32_t ld_bytes, depth;
     uint32_t from[DOWN ? 2 : kLoads];
     uint32_t at[DOWN ? T : 4];
 
     // rows m0 to m0 + 64 T; the wave multiplies those from `mine` on
     __device__ __forceinline__ Way(const Operand &o, uint32_t stack, uint32_t m0, uint32_t mine, uint32_t lane, uint32_t wave)
-        : base(static_cast<const char *>(o.p) + (stack * o.apart + (DOWN ? (size_t)m0 : (size_t)m0 * o.ld)) * 2), ld_bytes(o.ld * 2), depth(o.depth) {
+        : base(static_cast<const char *>(o.p) + (stack * o.apart + (DOWN ? (size_t)m0 : (size_t)m0 * o.ld)) * 2),
+          end(o.bytes ? reinterpret_cast<uint64_t>(o.p) + o.bytes : ~0ull), ld_bytes(o.ld * 2), depth(o.depth) {
         const uint32_t last = o.rows - 1 - m0;
         if constexpr (DOWN) {
             const uint32_t k = wave * kPerLoad + lane / (64 / kPerLoad), place = lane % (64 / kPerLoad);
@@ -142,7 +147,7 @@ struct Way {
             offset = from[i];
             behind = (size_t)step * kStep * 2 + lo;
         }
-        load_to_lds(base, behind, offset, (uint32_t)reinterpret_cast<uintptr_t>((Lds)lds) + place + (wave + 4 * i) * 1024);
+        load_to_lds(base, behind, end, offset, (uint32_t)reinterpret_cast<uintptr_t>((Lds)lds) + place + (wave + 4 * i) * 1024);
     }
     // block i (32 rows) of quarter j (16 of the k): lanes below 32 have k 8 j to 8 j + 7 of the step, the others those 32 further on
     __device__ __forceinline__ u32x4 read(const char *lds, int i, int j, uint32_t place) const {
@@ -192,7 +197,7 @@ __device__ __forceinline__ void store_out(void *to, bool bf16, size_t at, const 
 }
 
 // What becomes of eight neighbouring sums, as an End says it: load() brings what it takes besides (None where that is nothing), finish() computes, put() writes.  kStrips: it is given
-// them so, and not a wave's whole tile; kParts: the sum over k may come in parts; kSymmetric: the result may be computed by half.
+// them so, and not a wave's whole tile; kParts: the sum over k may come in parts; kSymmetric: the result may be computed by half; kRagged: b's last step along k is not whole.
 struct None {};
 
 // Tiles of 2 x 2 waves, each 32 T rows by 32 T columns of the result.  A step is 64 of k, multiplied in four quarters; the fragments of the
@@ -244,6 +249,16 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
         else f.a[i - T] = wa.read(lds, i - T, j, a);
     };
     f32x16 c[T][T] = {};
+    // b's k beyond the last one, which a's zeros alone would not undo: they may be NaN
+    u32x4 kept[4];
+    auto keep = [&](Fragments<T> &f, int j) {
+        if constexpr (End::kRagged)
+#pragma unroll
+            for (int i = 0; i < T; ++i) f.b[i] &= kept[j];
+    };
+    if constexpr (End::kRagged)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) kept[j] = u32x4{~0u, ~0u, ~0u, ~0u};
     if (from < to) {
         Fragments<T> f0, f1;
         uint32_t a = 0, b = kUnit, a1 = 2 * kUnit, b1 = 3 * kUnit, free = 4 * kUnit;     // places of this step's operands, the next one's, and of what comes next
@@ -260,6 +275,17 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
         __builtin_amdgcn_sched_barrier(0);
         for (uint32_t step = from; step < to; ++step) {
             const At coming = step_of(step + 2);
+            if constexpr (End::kRagged) {
+                if (step + 1 == to)
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+                        for (uint32_t d = 0; d < 4; ++d) {
+                            const uint32_t k = 32 * q + 8 * j + 2 * d;
+                            kept[j][d] = k + 1 < p.tail ? ~0u : k < p.tail ? 0xFFFFu : 0u;
+                        }
+            }
+            keep(f0, 0);
             // Part by part, with a read and perhaps a load in each: in one go they would keep the matrix unit waiting while their queues are full
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
@@ -267,6 +293,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
                 multiply<E>(c, f0, part);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            keep(f1, 1);
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
                 read(f0, part, 2, a, b);
@@ -274,6 +301,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
                 multiply<E>(c, f1, part);
                 __builtin_amdgcn_sched_barrier(0);
             }
+            keep(f0, 2);
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
                 read(f1, part, 3, a, b);
@@ -285,6 +313,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
             arrived<L>();
             __builtin_amdgcn_s_barrier();
             __builtin_amdgcn_sched_barrier(0);
+            keep(f1, 3);
 #pragma unroll
             for (int part = 0; part < 2 * T; ++part) {
                 read(f0, part, 0, a1, b1);

@@ -21,35 +21,43 @@ struct Plan {
 
 inline size_t bands_of(size_t tiles) { return (tiles + kHigh - 1) / kHigh; }
 
-// What a launch takes by its shape, from products of 64 to 8192 squared by 64 to 16384, as they lie and down k alike: us a step of 64 of k with few blocks on the card
+// What a product takes with a plan, from products of 64 to 8192 squared by 64 to 16384, as they lie and down k alike: us a step of 64 of k with few blocks on the card
 // and with as many as fit, and us a block besides, for its first loads and for writing the result.  Two launches cost 3 us more, and the partial sums their bytes, written, read
 // and joined at 2.5 TB/s.  us by tiles of 256 / 128 / 64 squared: 4096 cubed 103 / 121 / 200, 2048 cubed 40.6 / 21.6 / 30.3, 1024 cubed 23.5 / 9.6 / 6.2.
+struct Shape {
+    int tile;
+    double fit, empty, alone, full, starts, ends;      // empty: blocks a compute unit up to which a step takes as long as alone
+};
+constexpr Shape kShapes[] = {{4, 1, 0, 0.86, 1.40, 3.0, 9.0}, {2, 2, 0, 0.32, 0.87, 2.5, 2.5}, {1, 4, 1, 0.20, 0.80, 2.2, 1.0}};
+
+inline double cost_of(size_t M, size_t N, size_t K, size_t count, const Plan &plan) {
+    const Shape &s = kShapes[plan.tile == 4 ? 0 : plan.tile == 2 ? 1 : 2];
+    const size_t steps = (K + kStep - 1) / kStep, side = tiles_of(M, s.tile), tiles = plan.half ? side * (side + 1) / 2 : side * tiles_of(N, s.tile);
+    const double blocks = (double)(tiles * count * plan.splits), each = (double)((steps + plan.splits - 1) / plan.splits);
+    auto round = [&](double load) {       // blocks a compute unit
+        const double crowd = std::fmax(0.0, (load - s.empty) / (s.fit - s.empty));
+        return each * (s.alone + (s.full - s.alone) * crowd) + s.starts + (plan.half ? 1.5 : 1.0) * s.ends * std::fmax(0.25, load / s.fit);
+    };
+    const double rounds = std::floor(blocks / (256 * s.fit)), rest = blocks / 256 - rounds * s.fit;
+    double us = rounds * round(s.fit) + (rest > 0 ? round(rest) : 0);
+    if (plan.splits > 1) us += 3.0 + (double)(count * plan.splits * M * N) * 8 / 5e6;
+    return us;
+}
+
 inline Plan plan_of(size_t M, size_t N, size_t K, size_t count, bool may_split, bool symmetric = false) {
     const size_t steps = (K + kStep - 1) / kStep;
-    constexpr struct {
-        int tile;
-        double fit, empty, alone, full, starts, ends;      // empty: blocks a compute unit up to which a step takes as long as alone
-    } kShapes[] = {{4, 1, 0, 0.86, 1.40, 3.0, 9.0}, {2, 2, 0, 0.32, 0.87, 2.5, 2.5}, {1, 4, 1, 0.20, 0.80, 2.2, 1.0}};
     Plan best{1, 1};
     double least = 1e300;
-    for (const auto &s : kShapes) {
-        const size_t side = tiles_of(M, s.tile), tiles = side * tiles_of(N, s.tile) * count;
+    auto consider = [&](const Plan &plan) {
+        const double us = cost_of(M, N, K, count, plan);
+        if (us < least) least = us, best = plan;
+    };
+    for (const Shape &s : kShapes) {
+        const size_t tiles = tiles_of(M, s.tile) * tiles_of(N, s.tile) * count;
+        consider({s.tile, 1});
+        if (symmetric && tiles > count) consider({s.tile, 1, true});
         // no more parts than fill the card once
-        for (size_t splits = symmetric && side > 1 ? 0 : 1; splits <= 1 || (may_split && splits * 2 <= steps && tiles * splits <= (size_t)(256 * s.fit)); splits = splits ? splits * 2 : 1) {
-            // splits 0: half of the tiles
-            const bool half = splits == 0;
-            if (half) splits = 1;
-            const double blocks = half ? (double)(side * (side + 1) / 2 * count) : (double)(tiles * splits), each = (double)((steps + splits - 1) / splits);
-            auto round = [&](double load) {       // blocks a compute unit
-                const double crowd = std::fmax(0.0, (load - s.empty) / (s.fit - s.empty));
-                return each * (s.alone + (s.full - s.alone) * crowd) + s.starts + (half ? 1.5 : 1.0) * s.ends * std::fmax(0.25, load / s.fit);
-            };
-            const double rounds = std::floor(blocks / (256 * s.fit)), rest = blocks / 256 - rounds * s.fit;
-            double us = rounds * round(s.fit) + (rest > 0 ? round(rest) : 0);
-            if (splits > 1) us += 3.0 + (double)(count * splits * M * N) * 8 / 5e6;
-            if (us < least) least = us, best = Plan{s.tile, splits, half};
-            if (half) splits = 0;
-        }
+        for (size_t splits = 2; may_split && splits * 2 <= steps && tiles * splits <= (size_t)(256 * s.fit); splits *= 2) consider({s.tile, splits});
     }
     return best;
 }
@@ -62,6 +70,7 @@ struct Product {
     size_t count, M, N, steps;
     float *parts;              // as many as the plan asks for
     bool twofold = false;      // operands are sums of two
+    size_t tail = kStep;       // k of the last step
 };
 
 template <typename E, bool A_DOWN, bool B_DOWN, typename End>
@@ -69,7 +78,7 @@ int run(const Plan &plan, const Product &p, const typename End::Args &end, hipSt
     const size_t tiles_m = tiles_of(p.M, plan.tile), tiles_n = tiles_of(p.N, plan.tile), bands = plan.half ? bands_of(tiles_m) : 0;
     const size_t blocks = (bands ? half_tiles((uint32_t)tiles_m, (uint32_t)bands) : tiles_m * tiles_n) * plan.splits * p.count;
     if (blocks > kMaxBlocks) return SS_ERR_ARG;
-    const TilesArgs<typename End::Args> args{p.a, p.b, (uint32_t)p.M, (uint32_t)p.N, (uint32_t)(p.twofold ? 3 * p.steps : p.steps), (uint32_t)p.steps, (uint32_t)tiles_m, (uint32_t)tiles_n, (uint32_t)plan.splits, (uint32_t)bands, p.parts, end};
+    const TilesArgs<typename End::Args> args{p.a, p.b, (uint32_t)p.M, (uint32_t)p.N, (uint32_t)(p.twofold ? 3 * p.steps : p.steps), (uint32_t)p.tail, (uint32_t)p.steps, (uint32_t)tiles_m, (uint32_t)tiles_n, (uint32_t)plan.splits, (uint32_t)bands, p.parts, end};
     const auto kernel = plan.tile == 4 ? tiles_kernel<E, A_DOWN, B_DOWN, 4, End> : plan.tile == 2 ? tiles_kernel<E, A_DOWN, B_DOWN, 2, End> : tiles_kernel<E, A_DOWN, B_DOWN, 1, End>;
     const int rc = host::launch(kernel, blocks, 0, stream, args, 256);
     if (rc != SS_OK || plan.splits == 1) return rc;

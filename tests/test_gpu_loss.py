@@ -66,7 +66,8 @@ def test_loss_and_gradients(T, V, K):
     h, w, target, dloss = case(T, V, K)
     want = plain.softmax_loss(h, w, target, dloss)
     there = target >= 0
-    for pad, offset in ((0, 0), (3, 1), (8, 8)):
+    # rows at any multiple of 2, of 16 and of 4 bytes
+    for pad, offset in ((0, 0), (3, 1), (8, 8), (2 - K % 2, 2)):
         got = both(sliced(h, pad, offset), sliced(w, pad, offset), target.to(DEV), dloss.to(DEV), scratch_for(T, V, K), pad=pad, offset=offset)
         check(got, want, there)
         assert (got["loss"][~there.to(DEV)] == 0).all() and (got["dh"][~there.to(DEV)] == 0).all()

@@ -145,7 +145,7 @@ def kind(symbol):
 
 
 # what each kind of call meets: more than the GPU tests', for the sizes that these would take long with
-LARGE_LOSSES = [(8192, 128000, 4096), (8192, 8192, 8192), (4096, 32000, 2048), (2048, 2048, 2048), (300, 700, 192), (4096, 4096, 64), (64, 64, 64), (16, 256, 8192), (1024, 1024, 8192)]
+LARGE_LOSSES = [(8192, 128000, 4096), (8192, 128000, 4008), (900, 20000, 1002), (8192, 8192, 8192), (4096, 32000, 2048), (2048, 2048, 2048), (300, 700, 192), (4096, 4096, 64), (64, 64, 64), (16, 256, 8192), (1024, 1024, 8192)]
 LARGE_MATRICES = [(1, 8192, 8192), (1, 4096, 4096), (1, 2048, 2048), (1, 1024, 1024), (1, 512, 4096), (1, 4096, 512), (24, 512, 2048), (24, 2048, 512), (1, 20, 30), (1, 30, 800), (1, 90, 90), (1, 250, 80), (1, 130, 8192), (1, 8192, 130), (8, 4096, 8192),
                   (8, 8192, 4096), (1, 32768, 2048), (1, 2048, 32768)]
 
@@ -166,17 +166,17 @@ def check_every_kernel_is_reached(c):
 
 def check_gpu_tests_reach_both_sides(c):
     sizes, tiles, joins = gpu_loss.SIZES + gpu_loss.LARGE, {}, set()
-    pieces, copies = set(), set()
+    pieces, ragged = set(), set()
     for T, V, K in sizes:
         got = [kind(s) for call in (c.loss, c.grad) for s in c.of(call, T, V, K)]
         for name, ends, numbers in got:
             if name == "tiles_kernel":
-                tiles.setdefault(ends[0], set()).add(numbers[-1])
+                tiles.setdefault(ends[0], set()).add(numbers[2])
+                ragged.update({ends[0] + str(numbers[3])} if len(numbers) > 3 else ())
         joins.add(any(name == "join_kernel" for name, _, _ in got))
         pieces.add(min(2, sum(ends == ["SoftmaxEnd"] for _, ends, _ in got)))
-        copies.add(K % 64 == 0)
     assert tiles == {"StatsEnd": {1, 2, 4}, "SoftmaxEnd": {1, 2, 4}, "GradientEnd": {1, 2, 4}}, tiles
-    assert joins == {False, True} and pieces == {1, 2} and copies == {False, True}, (joins, pieces)
+    assert joins == {False, True} and pieces == {1, 2} and ragged == {"StatsEnd0", "StatsEnd1", "SoftmaxEnd0", "SoftmaxEnd1"}, (joins, pieces, ragged)
     tiles, whole, halves, twofold, joins = {}, set(), set(), set(), set()
     for rows, cols in gpu_orthogonal.SHAPES + gpu_orthogonal.LARGE:
         for call, how in ((c.orthogonalize, {"odt": BF16}), (c.orthogonalize, {"odt": F32}), (c.step, {})):
