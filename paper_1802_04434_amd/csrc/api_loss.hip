@@ -48,7 +48,7 @@ int along_weights(const Plan &plan, Product p, size_t K, bool copy, const typena
 
 // What is computed at a time is a piece of the vocabulary.  Forward: 2^36 entries of z, or 128 MB of copied weights.  Backward: 128 MB of D, so that
 // the products that read it find it in the memory-side cache.
-constexpr size_t kPieceEntries = (size_t)1 << 26, kForwardEntries = (size_t)1 << 36, kEdge = 256;
+constexpr size_t kPieceEntries = (size_t)1 << 28, kForwardEntries = (size_t)1 << 36, kEdge = 256;
 
 inline size_t piece_of(size_t entries, size_t rows, size_t V) { return std::min(std::max(entries / rows / kEdge * kEdge, 4 * kEdge), rounded(V, kEdge)); }
 

@@ -37,33 +37,35 @@ struct StatsEnd {
     // A wave's 32 T rows by 32 T columns of z; a row is in lanes r and r + 32, four columns of each eight
     template <int T>
     static __device__ __forceinline__ void finish(const Args &a, const f32x16 (&c)[T][T], uint32_t m, uint32_t n, uint32_t part, uint32_t M, uint32_t N, uint32_t r, uint32_t q) {
+        if (N >= n + 32 * T) rows<T, true>(a, c, m, n, part, M, N, r, q);
+        else rows<T, false>(a, c, m, n, part, M, N, r, q);
+    }
+    template <int T, bool INSIDE>
+    static __device__ __forceinline__ void rows(const Args &a, const f32x16 (&c)[T][T], uint32_t m, uint32_t n, uint32_t part, uint32_t M, uint32_t N, uint32_t r, uint32_t q) {
         const uint32_t left = N > n + 4 * q ? N - n - 4 * q : 0;      // columns from this lane's first one on: a part of none counts for nothing
 #pragma unroll
         for (int i = 0; i < T; ++i) {
             const uint32_t row = m + i * 32 + r;
             const bool there = row < M;
+            const int64_t target = there ? a.target[row] : -1;
             float top = -__builtin_inff();
 #pragma unroll
             for (int k = 0; k < T; ++k)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const uint32_t col = k * 32 + e / 4 * 8 + e % 4;
-                    if (col < left) top = fmaxf(top, c[i][k][e]);
-                }
+                for (int e = 0; e < 16; ++e)
+                    if (INSIDE || k * 32 + e / 4 * 8 + e % 4 < left) top = fmaxf(top, c[i][k][e]);
             top = fmaxf(top, __shfl_xor(top, 32));
-            // NaN passes: it is not the largest, but its exponential is NaN
+            // NaN passes: it is not the largest, but its exponential is NaN.  Where there is none but -infinity their exponentials are 0.
+            const float from = top == -__builtin_inff() ? 0.0f : top;
             float sum = 0;
 #pragma unroll
             for (int k = 0; k < T; ++k)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const uint32_t col = k * 32 + e / 4 * 8 + e % 4;
-                    const float z = c[i][k][e];
-                    if (col < left) sum += z == -__builtin_inff() ? 0.0f : exp_of(z - top);
-                }
+                for (int e = 0; e < 16; ++e)
+                    if (INSIDE || k * 32 + e / 4 * 8 + e % 4 < left) sum += exp_of(c[i][k][e] - from);
             sum += __shfl_xor(sum, 32);
             if (there && q == 0) a.parts[(size_t)(a.part0 + part) * M + row] = Part{top, sum};
-            const int64_t hit = there ? a.target[row] - a.first - n - 4 * q : -1;
+            const int64_t hit = target < 0 ? -1 : target - a.first - n - 4 * q;
             if (hit >= 0 && hit < 32 * T && hit < left) {
 #pragma unroll
                 for (int k = 0; k < T; ++k)
@@ -192,12 +194,17 @@ struct SoftmaxEnd {
         return row < a.T ? Besides{a.lse[row], a.factor[row], a.target[row]} : Besides{0, 0, -1};
     }
     static __device__ __forceinline__ void finish(const Args &a, const Besides &b, uint32_t, uint32_t col, f32x4 (&v)[2]) {
-        const int64_t hit = b.target - a.first - col;
+        const uint64_t behind = (uint64_t)(b.target - a.first - col);
+        const uint32_t hit = b.target >= 0 && behind < 8 ? (uint32_t)behind : 8u;
 #pragma unroll
         for (int x = 0; x < 8; ++x) {
             const float p = exp_of(v[x / 4][x % 4] - b.lse);
-            v[x / 4][x % 4] = b.target >= 0 && col + x < a.vocab ? b.factor * (hit == x ? p - 1.0f : p) : 0.0f;
+            v[x / 4][x % 4] = b.factor * (hit == x ? p - 1.0f : p);
         }
+        if (b.target < 0 || col + 8 > a.vocab)      // NaN times zero would not be zero
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+                if (b.target < 0 || col + x >= a.vocab) v[x / 4][x % 4] = 0.0f;
     }
     static __device__ __forceinline__ void put(const Args &a, uint32_t, uint32_t row, uint32_t col, const f32x4 (&v)[2], uint32_t) {
         product::bf16x8 o;

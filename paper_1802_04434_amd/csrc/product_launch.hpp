@@ -28,7 +28,7 @@ struct Shape {
     int tile;
     double fit, empty, alone, full, starts, ends;      // empty: blocks a compute unit up to which a step takes as long as alone
 };
-constexpr Shape kShapes[] = {{4, 1, 0, 0.86, 1.40, 3.0, 9.0}, {2, 2, 0, 0.32, 0.87, 2.5, 2.5}, {1, 4, 1, 0.20, 0.80, 2.2, 1.0}};
+constexpr Shape kShapes[] = {{4, 1, 0, 0.90, 1.40, 3.0, 9.0}, {2, 2, 0, 0.38, 0.87, 2.5, 2.5}, {1, 4, 0.5, 0.25, 0.80, 2.2, 1.0}};
 
 inline double cost_of(size_t M, size_t N, size_t K, size_t count, const Plan &plan) {
     const Shape &s = kShapes[plan.tile == 4 ? 0 : plan.tile == 2 ? 1 : 2];
