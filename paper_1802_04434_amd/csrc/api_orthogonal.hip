@@ -35,6 +35,28 @@ inline size_t norm_blocks(const Stack &s) { return std::min(std::max((s.rows * s
 // by, of the result's norm, without / with: 40 x 40 1.1e-3 / 1e-4, 257 x 300 FEW_A, 512 squared 6e-4 / 4e-4, 1024 x 2048 4e-4.
 inline int twofold_steps(size_t shorter, bool fp32) { return !fp32 || shorter >= 1024 ? 0 : shorter >= 512 ? 1 : shorter >= 256 ? 2 : 3; }
 
+// a shorter side of 128 at most, and slices of the longer one
+struct Slices {
+    size_t shorter, slice, count;      // count 0: another way is taken
+    explicit Slices(const Stack &s) : shorter(rounded(std::min(s.rows, s.cols), 32)), slice(shorter <= 64 ? 128 : 64), count((std::max(s.rows, s.cols) + slice - 1) / slice) {
+        if (shorter > 128 || count > 1024) count = 0;
+    }
+};
+
+struct SlicePlace {
+    size_t sums, hi, lo, a_hi, a_lo, parts, bytes;
+    SlicePlace(const Stack &s, const Slices &t) {
+        Layout l;
+        sums = l.take(s.count * norm_blocks(s) * sizeof(double));
+        hi = l.take(s.count * t.count * t.slice * t.shorter * 2);
+        lo = l.take(s.count * t.count * t.slice * t.shorter * 2);
+        a_hi = l.take(s.count * t.shorter * t.shorter * 2);
+        a_lo = l.take(s.count * t.shorter * t.shorter * 2);
+        parts = l.take(s.count * t.count * t.shorter * t.shorter * sizeof(float));
+        bytes = l.bytes;
+    }
+};
+
 struct Plans {
     Plan square, polynomial, update;
 };
@@ -70,6 +92,11 @@ struct Place {
     }
 };
 
+inline size_t scratch_of(const Stack &s) {
+    const Slices slices(s);
+    return slices.count ? SlicePlace(s, slices).bytes : Place(s).bytes;
+}
+
 // a gradient on its way into an update, and where the update goes
 struct Ends {
     const void *g;
@@ -92,6 +119,8 @@ inline bool fits(const Stack &s) {
     return shorter <= 128 && longer / 32 * (shorter / 32) <= kTiles && orthogonal::whole_bytes((uint32_t)shorter, (uint32_t)longer) <= orthogonal::kWholeBytes;
 }
 
+inline float mu_of(int step, int steps) { return step + 1 == steps ? orthogonal::kLast : step + 2 == steps ? orthogonal::kBefore : 0.0f; }
+
 // two blocks on a compute unit where its LDS has room for them
 inline auto whole(uint32_t shorter, bool half) {
     using namespace orthogonal;
@@ -112,8 +141,26 @@ int orthogonalized(const Stack &s, const Ends &e, int steps, char *scratch, hipS
         const auto kernel = whole(std::min(rows, cols), bytes <= kWholeHalf);
         return launch(kernel, s.count, 0, stream, a, 64 * kWholeWaves);
     }
-    const Place place(s);
     const size_t blocks = norm_blocks(s);
+    if (const Slices slices(s); slices.count) {
+        const SlicePlace place(s, slices);
+        auto half = [&](size_t at) { return reinterpret_cast<_Float16 *>(scratch + at); };
+        float *parts = reinterpret_cast<float *>(scratch + place.parts);
+        const BeginArgs begin{e.g, e.m, reinterpret_cast<double *>(scratch + place.sums), half(place.hi), half(place.lo), e.ld, e.apart, (uint32_t)s.rows, (uint32_t)s.cols, 0, 0,
+                              (uint32_t)blocks, e.beta, e.gdt == SS_BF16, e.ahead, e.ld == s.cols || s.rows == 1};
+        int rc = launch(norm_kernel, blocks, 0, stream, begin, 256, (int)s.count);
+        const uint32_t size = (uint32_t)(slices.shorter * slices.shorter);
+        const auto kernel = slices.shorter == 32 ? slice_kernel<32> : slices.shorter == 64 ? slice_kernel<64> : slices.shorter == 96 ? slice_kernel<96> : slice_kernel<128>;
+        for (int k = -1; rc == SS_OK && k < steps; ++k) {
+            const SliceArgs a{begin, k < 0 ? nullptr : half(place.a_hi), half(place.a_lo), parts, k + 1 == steps ? e.out : nullptr, e.ldo, e.aparto, e.delta, mu_of(k, steps), (uint32_t)slices.count,
+                              e.step, e.odt == SS_BF16};
+            rc = launch(kernel, slices.count, 0, stream, a, 64 * kWholeWaves, (int)s.count);
+            if (rc == SS_OK && k + 1 < steps)
+                rc = launch(sum_kernel, size / 64, 0, stream, SumArgs{parts, half(place.a_hi), half(place.a_lo), size, (uint32_t)slices.count}, 256, (int)s.count);
+        }
+        return rc;
+    }
+    const Place place(s);
     auto half = [&](size_t at) { return reinterpret_cast<_Float16 *>(scratch + at); };
     _Float16 *hi[2] = {half(place.hi[0]), half(place.hi[1])}, *lo[2] = {half(place.lo[0]), half(place.lo[1])}, *a[2] = {half(place.a[0]), half(place.a[1])}, *b[2] = {half(place.b[0]), half(place.b[1])};
     float *parts = reinterpret_cast<float *>(scratch + place.parts);
@@ -129,7 +176,7 @@ int orthogonalized(const Stack &s, const Ends &e, int steps, char *scratch, hipS
     const int precise = twofold_steps(place.shorter, e.odt == SS_F32);
     for (int k = 0; k < steps; ++k) {
         const bool last = k + 1 == steps, twofold = k + precise >= steps;
-        const float mu = last ? kLast : k + 2 == steps ? kBefore : 0.0f;
+        const float mu = mu_of(k, steps);
         const int at = k & 1, next = ~k & 1;
         const Plans &plans = twofold ? place.twofold : place.once;
         const Operand x{hi[at], C, R, R, whole, lo[at] - hi[at], 0}, down{hi[at], C, C, R, whole, lo[at] - hi[at], 0}, as{a[0], S, S, S, square, a[1] - a[0], 0}, bs{b[0], S, S, S, square, b[1] - b[0], 0};
@@ -154,7 +201,7 @@ extern "C" {
 
 size_t ss_orthogonalize_scratch_bytes(size_t count, size_t rows, size_t cols) {
     const Stack s{count, rows, cols};
-    return s.empty() || s.bad() ? 0 : Place(s).bytes;
+    return s.empty() || s.bad() ? 0 : scratch_of(s);
 }
 
 int ss_orthogonalize(const void *g, ss_dtype gdt, size_t count, size_t rows, size_t cols, size_t ld, size_t apart, int steps, void *out, ss_dtype odt, size_t ldo,
@@ -167,7 +214,7 @@ int ss_orthogonalize(const void *g, ss_dtype gdt, size_t count, size_t rows, siz
     if (!g || !out || !scratch) return SS_ERR_NULL;
     if (!element_aligned(g, gdt) || !element_aligned(out, odt) || !aligned16(scratch)) return SS_ERR_ALIGN;
     Span spans[3] = {s.of(g, ld, apart, gdt, false), s.of(out, ldo, aparto, odt, true), span(scratch, scratch_bytes, true)};
-    if (written_spans_overlap(spans, 3) || scratch_bytes < Place(s).bytes) return SS_ERR_ARG;
+    if (written_spans_overlap(spans, 3) || scratch_bytes < scratch_of(s)) return SS_ERR_ARG;
     return orthogonalized(s, {g, gdt, ld, apart, nullptr, 0, false, out, odt, ldo, aparto, 0, false}, steps, static_cast<char *>(scratch), static_cast<hipStream_t>(hip_stream));
 }
 
@@ -181,7 +228,7 @@ int ss_orthogonal_step(const void *g, ss_dtype gdt, size_t count, size_t rows, s
     if (!g || !m || !x || !scratch) return SS_ERR_NULL;
     if (!element_aligned(g, gdt) || !element_aligned(m, SS_F32) || !element_aligned(x, SS_F32) || !aligned16(scratch)) return SS_ERR_ALIGN;
     Span spans[4] = {s.of(g, ld, apart, gdt, false), s.of(m, cols, rows * cols, SS_F32, true), s.of(x, cols, rows * cols, SS_F32, true), span(scratch, scratch_bytes, true)};
-    if (written_spans_overlap(spans, 4) || scratch_bytes < Place(s).bytes) return SS_ERR_ARG;
+    if (written_spans_overlap(spans, 4) || scratch_bytes < scratch_of(s)) return SS_ERR_ARG;
     return orthogonalized(s, {g, gdt, ld, apart, m, beta, ahead == 1, x, SS_F32, cols, rows * cols, delta, true}, steps, static_cast<char *>(scratch),
                           static_cast<hipStream_t>(hip_stream));
 }

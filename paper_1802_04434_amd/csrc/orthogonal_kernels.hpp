@@ -332,7 +332,7 @@ __device__ __forceinline__ f32x16 whole_tile(const char *mh, const char *ml, uin
 }
 
 // four neighbours as hi + lo
-__device__ __forceinline__ void put_four(char *hi, char *lo, uint32_t at, const f32x4 &v) {
+__device__ __forceinline__ void put_four(char *hi, char *lo, size_t at, const f32x4 &v) {
     f16x4 h, l;
 #pragma unroll
     for (int x = 0; x < 4; ++x) h[x] = (_Float16)v[x], l[x] = (_Float16)(v[x] - (float)h[x]);
@@ -477,6 +477,162 @@ __global__ __launch_bounds__(64 * kWholeWaves) void whole_kernel(const WholeArgs
         }
         product::store_out(p.out, p.bf16, to, v, n);
     }
+}
+
+// ------------------------------------------------------------ long matrices with a short side, in slices ----
+// With a shorter side of 128 at most, B is so small that every block computes it for itself: a block has a slice of X's longer side in LDS, makes B of A there, its slice of the next X, and that
+// slice's part of the next A, so that a step takes two launches instead of three or four: this, and the one that adds the parts.  Both X and A have 22 bits, as above.
+// SLICE_FIGURES
+template <uint32_t S>
+constexpr uint32_t kSlice = S <= 64 ? 128 : 64;      // of the longer side: one eight of a row of g, and one tile of 32 squared a wave
+
+struct SliceArgs {
+    BeginArgs begin;               // hi, lo: (stack, slices, kSlice, S)
+    const _Float16 *a_hi, *a_lo;   // (stack, S, S); NULL the first time, when the slice comes from g
+    float *parts;                  // (stack, slices, S, S)
+    void *out;                     // NULL: not the last time
+    uint64_t ld, apart;
+    float delta, mu;
+    uint32_t slices;
+    bool step, bf16;
+};
+
+// rows of S entries between memory and LDS
+template <uint32_t S>
+__device__ __forceinline__ void bring_rows(char *lds, const _Float16 *from, uint32_t rows) {
+    for (uint32_t at = threadIdx.x; at < rows * (S / 8); at += 64 * kWholeWaves)
+        *reinterpret_cast<u32x4 *>(lds + place<S>(at / (S / 8), at % (S / 8) * 8)) = *reinterpret_cast<const u32x4 *>(from + at * 8);
+}
+template <uint32_t S>
+__device__ __forceinline__ void take_rows(const char *lds, _Float16 *to, uint32_t rows) {
+    for (uint32_t at = threadIdx.x; at < rows * (S / 8); at += 64 * kWholeWaves)
+        *reinterpret_cast<u32x4 *>(to + at * 8) = *reinterpret_cast<const u32x4 *>(lds + place<S>(at / (S / 8), at % (S / 8) * 8));
+}
+
+template <uint32_t S>
+__global__ __launch_bounds__(64 * kWholeWaves) void slice_kernel(const SliceArgs p) {
+    constexpr uint32_t W = kSlice<S>, kX = W * S * 2, kSquare = S * S * 2, across = S / 32;
+    static_assert(across * across <= kWholeWaves && W / 32 * across <= kWholeWaves && W * S / 8 <= 64 * kWholeWaves, "one tile a wave, one eight a thread");
+    __shared__ __attribute__((aligned(16))) char lds[2 * (kX + kSquare)];
+    __shared__ double shared[kWholeWaves];
+    char *const xh = lds, *const xl = xh + kX, *const ah = xl + kX, *const al = ah + kSquare;
+    const BeginArgs &a = p.begin;
+    const uint32_t slice = blockIdx.x, stack = blockIdx.y, lane = threadIdx.x & 63u, wave = product::uniform(threadIdx.x >> 6), r = lane & 31u, q = lane >> 5;
+    const bool tall = a.rows > a.cols;
+    // this thread's eight of g: of a row of the slice, or of a row's part that belongs to it
+    const uint32_t eights = tall ? (a.cols + 7) / 8 : W / 8, line = threadIdx.x / eights, first = threadIdx.x % eights * 8;
+    const uint32_t row = tall ? slice * W + line : line, col = tall ? first : slice * W + first;
+    const bool mine = (tall ? line < W : true) && row < a.rows && col < a.cols;
+    const uint32_t n = mine ? a.cols - col : 0;
+    auto entry = [&](uint32_t x) { return tall ? place<S>(line, first + x) : place<S>(first + x, line); };
+    _Float16 *const hi = a.hi + ((size_t)stack * p.slices + slice) * W * S, *const lo = a.lo + ((size_t)stack * p.slices + slice) * W * S;
+    if (!p.a_hi) {
+        float g[8] = {}, m[8] = {};
+        if (mine) {
+            load_eight(g, a.g, a.bf16, stack * a.apart + row * a.ld + col, n);
+            if (a.m) load_eight(m, a.m, false, ((size_t)stack * a.rows + row) * a.cols + col, n);
+        }
+        double sum = 0;
+        for (uint32_t k = threadIdx.x; k < a.blocks; k += 64 * kWholeWaves) sum += a.sums[(size_t)stack * a.blocks + k];
+        sum = ss::sum_wave(sum);
+        if (lane == 63) shared[wave] = sum;
+        for (uint32_t at = threadIdx.x * 16; at < 2 * kX; at += 64 * kWholeWaves * 16) *reinterpret_cast<u32x4 *>(lds + at) = u32x4{0, 0, 0, 0};
+        __syncthreads();
+        sum = 0;
+        for (int k = 0; k < kWholeWaves; ++k) sum += shared[k];
+        const Scale scale(sum);
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x)
+            if (x < n) {
+                const float v = scale(update_of(a, g[x], m[x]));
+                const _Float16 h = (_Float16)v;
+                *reinterpret_cast<_Float16 *>(xh + entry(x)) = h;
+                *reinterpret_cast<_Float16 *>(xl + entry(x)) = (_Float16)(v - (float)h);
+            }
+        __syncthreads();
+    } else {
+        bring_rows<S>(xh, hi, W);
+        bring_rows<S>(xl, lo, W);
+        bring_rows<S>(ah, p.a_hi + (size_t)stack * S * S, S);
+        bring_rows<S>(al, p.a_lo + (size_t)stack * S * S, S);
+        __syncthreads();
+        // B + mu I in A's place, then X <- (a - mu) X + X (B + mu I)
+#pragma unroll 1
+        for (int x_too = 0; x_too < 2; ++x_too) {
+            char *const ph = x_too ? xh : ah, *const pl = x_too ? xl : al;
+            const float was_by = x_too ? ::orthogonal::kA - p.mu : kB, sum_by = x_too ? kUnscale : kC * kUnscale, diagonal = x_too ? 0.0f : p.mu * kScale;
+            const bool busy = wave < (x_too ? W / 32 * across : across * across);
+            const uint32_t m = wave / across * 32, n0 = wave % across * 32;
+            f32x16 c = {};
+            if (busy) {
+                c = whole_tile<S, false>(ph, pl, m, ah, al, n0, S, lane);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x4 was = get_four(ph, pl, place<S>(m + r, n0 + 8 * e + 4 * q));
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) c[4 * e + x] = __builtin_fmaf(was_by, was[x], c[4 * e + x] * sum_by);
+                }
+                if (m == n0 && diagonal != 0.0f)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (r == e / 4 * 8 + 4 * q + e % 4) c[e] += diagonal;
+            }
+            __syncthreads();
+            if (busy)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) put_four(ph, pl, place<S>(m + r, n0 + 8 * e + 4 * q), f32x4{c[4 * e], c[4 * e + 1], c[4 * e + 2], c[4 * e + 3]});
+            __syncthreads();
+        }
+    }
+    if (p.out) {
+        if (!mine) return;
+        f32x4 v[2];
+#pragma unroll
+        for (uint32_t x = 0; x < 8; ++x) {
+            const uint32_t at = x < n ? entry(x) : 0;
+            v[x / 4][x % 4] = ((float)*reinterpret_cast<const _Float16 *>(xh + at) + (float)*reinterpret_cast<const _Float16 *>(xl + at)) * kUnscale;
+        }
+        const size_t to = stack * p.apart + row * p.ld + col;
+        if (p.step) {
+            float was[8];
+            load_eight(was, p.out, false, to, n);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) v[x / 4][x % 4] = was[x] - p.delta * v[x / 4][x % 4];
+        }
+        product::store_out(p.out, p.bf16, to, v, n);
+        return;
+    }
+    take_rows<S>(xh, hi, W);
+    take_rows<S>(xl, lo, W);
+    if (wave >= across * across) return;
+    const uint32_t m = wave / across * 32, n0 = wave % across * 32;
+    const f32x16 c = whole_tile<S, true>(xh, xl, m, xh, xl, n0, W, lane);
+    float *to = p.parts + ((size_t)stack * p.slices + slice) * S * S + (m + r) * S + n0 + 4 * q;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) *reinterpret_cast<f32x4 *>(to + 8 * e) = f32x4{c[4 * e], c[4 * e + 1], c[4 * e + 2], c[4 * e + 3]};
+}
+
+struct SumArgs {
+    const float *parts;
+    _Float16 *hi, *lo;
+    uint32_t size, slices;         // S x S; parts of each
+};
+
+// A of its parts: 16 threads share four neighbours' parts, in an order that depends on their number alone
+__global__ __launch_bounds__(256) void sum_kernel(const SumArgs p) {
+    __shared__ f32x4 shared[16][17];
+    const uint32_t four = blockIdx.x * 16 + (threadIdx.x & 15u), share = threadIdx.x >> 4, stack = blockIdx.y;
+    const float *from = p.parts + (size_t)stack * p.slices * p.size + four * 4;
+    f32x4 s = {0, 0, 0, 0};
+#pragma unroll 8
+    for (uint32_t k = share; k < p.slices; k += 16) s += *reinterpret_cast<const f32x4 *>(from + (size_t)k * p.size);
+    shared[threadIdx.x & 15u][share] = s;
+    __syncthreads();
+    if (threadIdx.x >= 16) return;
+    s = shared[threadIdx.x][0];
+    for (int k = 1; k < 16; ++k) s += shared[threadIdx.x][k];
+    const size_t at = ((size_t)stack * p.size + four * 4) * sizeof(_Float16);
+    put_four(reinterpret_cast<char *>(p.hi), reinterpret_cast<char *>(p.lo), at, s * kUnscale);
 }
 
 }  // namespace orthogonal
