@@ -32,14 +32,16 @@ inline bool element_aligned(const void *p, ss_dtype dt) { return reinterpret_cas
 inline size_t norm_blocks(const Stack &s) { return std::min(std::max((s.rows * s.cols + 2047) / 2048, (size_t)1), std::max((size_t)1024 / s.count, (size_t)1)); }
 
 // How many of the last steps multiply operands of 22 bits, in three products of 11: where the result is fp32, and the matrix so short that its roundings do not average out.  Off
-// by, of the result's norm, without / with: 40 x 40 1.1e-3 / 1e-4, 257 x 300 FEW_A, 512 squared 6e-4 / 4e-4, 1024 x 2048 4e-4.
+// by, of the result's norm, without / with: 40 x 40 1.1e-3 / 1e-4, 120 x 1000 7.9e-4 / 1e-4, 512 squared 6.1e-4 / 3.9e-4, 1024 x 2048 4.2e-4.
 inline int twofold_steps(size_t shorter, bool fp32) { return !fp32 || shorter >= 1024 ? 0 : shorter >= 512 ? 1 : shorter >= 256 ? 2 : 3; }
 
-// a shorter side of 128 at most, and slices of the longer one
+// A shorter side of 128 at most, and slices of the longer one.  A block of 96 and 128 has a compute unit to itself and makes B as every other one does: many of them take longer than the
+// products in tiles.  us, in slices / in tiles to bf16 / to fp32: 25 x 7616 48 / 90 / 100, 64 x 64000 115 / 128 / 151, 1000 x 120 73 / 89 / 100, 128 x 8128 102 / 100 / 120, 128 x 16000 122 / 114 /
+// 135, 128 x 60000 304 / 170 / 213; 25 of 1000 x 120 167 / 121 / 148.
 struct Slices {
     size_t shorter, slice, count;      // count 0: another way is taken
     explicit Slices(const Stack &s) : shorter(rounded(std::min(s.rows, s.cols), 32)), slice(shorter <= 64 ? 128 : 64), count((std::max(s.rows, s.cols) + slice - 1) / slice) {
-        if (shorter > 128 || count > 1024) count = 0;
+        if (shorter > 128 || count > 1024 || (shorter > 64 && s.count * count * shorter * shorter > (size_t)1 << 21)) count = 0;
     }
 };
 
@@ -112,11 +114,12 @@ struct Ends {
     bool step;
 };
 
-// whether a matrix fits into LDS as it is worked on there
+// Whether a matrix is worked on whole, by one block.  It has to fit into LDS, and one block sums over the longer side alone.  us, whole / in slices, any type: 64 x 64 18 / 49, 64 x 300
+// 46 / 50, 64 x 480 65 / 50, 32 x 300 29 / 41, 32 x 900 65 / 43, 128 x 128 50 / 71; 48 of 64 x 300 47 / 63.
 inline bool fits(const Stack &s) {
     const size_t shorter = rounded(std::min(s.rows, s.cols), 32), longer = rounded(std::max(s.rows, s.cols), 32);
     constexpr size_t kTiles = orthogonal::kWholeWaves * orthogonal::kWholeTiles;
-    return shorter <= 128 && longer / 32 * (shorter / 32) <= kTiles && orthogonal::whole_bytes((uint32_t)shorter, (uint32_t)longer) <= orthogonal::kWholeBytes;
+    return shorter <= 128 && longer <= 320 && longer / 32 * (shorter / 32) <= kTiles && orthogonal::whole_bytes((uint32_t)shorter, (uint32_t)longer) <= orthogonal::kWholeBytes;
 }
 
 inline float mu_of(int step, int steps) { return step + 1 == steps ? orthogonal::kLast : step + 2 == steps ? orthogonal::kBefore : 0.0f; }
@@ -125,7 +128,7 @@ inline float mu_of(int step, int steps) { return step + 1 == steps ? orthogonal:
 inline auto whole(uint32_t shorter, bool half) {
     using namespace orthogonal;
     switch (shorter) {
-        case 32: return half ? whole_kernel<32, kWholeHalf> : whole_kernel<32, kWholeBytes>;
+        case 32: return whole_kernel<32, kWholeHalf>;
         case 64: return half ? whole_kernel<64, kWholeHalf> : whole_kernel<64, kWholeBytes>;
         case 96: return half ? whole_kernel<96, kWholeHalf> : whole_kernel<96, kWholeBytes>;
         default: return whole_kernel<128, kWholeBytes>;      // A alone has 64 KB, X as much

@@ -14,7 +14,7 @@ SIZES = [(1, 1, 1), (1, 2, 64), (1, 1000, 8), (2, 63, 7), (3, 64, 64), (5, 65, 6
          (65, 129, 72), (100, 33, 200), (127, 513, 130), (128, 1000, 256), (129, 2049, 40), (257, 300, 520), (300, 700, 192), (513, 96, 320)]
 
 # every tile size, several pieces of the vocabulary (also of copied weights), sums in parts; compared with 64 bits on the GPU
-LARGE = [(1, 70_001, 64), (2, 30_000, 200), (40, 257, 8192), (1500, 4100, 256), (2600, 5000, 320), (5000, 9000, 1000), (33_000, 2200, 72), (3, 1500, 60_001)]
+LARGE = [(1, 70_001, 64), (2, 30_000, 200), (40, 257, 8192), (1500, 4100, 256), (2600, 5000, 320), (5000, 9000, 1000), (33_000, 9000, 72), (3, 5000, 60_001)]
 
 
 def sliced(x, pad, offset):

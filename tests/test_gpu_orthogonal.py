@@ -13,8 +13,8 @@ DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
 # one entry to several tiles, wide, tall and square, both sides of 8, 64, 128 and 256
 SHAPES = [(1, 1), (1, 7), (9, 1), (1, 500), (3, 5), (8, 64), (63, 65), (64, 64), (65, 33), (70, 90), (100, 300), (129, 128), (257, 40), (200, 257), (260, 260), (96, 1100), (700, 130)]
 
-# each number of steps in 22 bits, halves of symmetric products of every tile size, sums in parts
-LARGE = [(300, 700), (600, 520), (530, 2000), (2050, 1030), (140, 5000), (5000, 300), (2100, 2200), (3000, 3100)]
+# slices of either side, each number of steps in 22 bits, halves of symmetric products of every tile size, sums in parts
+LARGE = [(20, 4000), (5000, 50), (90, 2000), (1500, 120), (100, 20_000), (64, 140_000), (300, 700), (600, 520), (530, 2000), (2050, 1030), (140, 5000), (5000, 300), (2100, 2200), (3000, 3100)]
 
 
 def matrix(rows, cols, seed=0, kind="gradient"):

@@ -146,7 +146,7 @@ def kind(symbol):
 
 # what each kind of call meets: more than the GPU tests', for the sizes that these would take long with
 LARGE_LOSSES = [(8192, 128000, 4096), (8192, 128000, 4008), (900, 20000, 1002), (8192, 8192, 8192), (4096, 32000, 2048), (2048, 2048, 2048), (300, 700, 192), (4096, 4096, 64), (64, 64, 64), (16, 256, 8192), (1024, 1024, 8192)]
-LARGE_MATRICES = [(1, 8192, 8192), (1, 4096, 4096), (1, 2048, 2048), (1, 1024, 1024), (1, 512, 4096), (1, 4096, 512), (24, 512, 2048), (24, 2048, 512), (1, 20, 30), (1, 30, 800), (1, 90, 90), (1, 250, 80), (1, 130, 8192), (1, 8192, 130), (8, 4096, 8192),
+LARGE_MATRICES = [(1, 8192, 8192), (1, 4096, 4096), (1, 2048, 2048), (1, 1024, 1024), (1, 512, 4096), (1, 4096, 512), (24, 512, 2048), (24, 2048, 512), (1, 20, 30), (1, 30, 800), (1, 90, 90), (1, 250, 80), (1, 100, 30), (1, 60, 300), (1, 130, 8192), (1, 128, 100_000), (1, 100_000, 128), (1, 8192, 130), (8, 4096, 8192),
                   (8, 8192, 4096), (1, 32768, 2048), (1, 2048, 32768)]
 
 
@@ -177,23 +177,25 @@ def check_gpu_tests_reach_both_sides(c):
         pieces.add(min(2, sum(ends == ["SoftmaxEnd"] for _, ends, _ in got)))
     assert tiles == {"StatsEnd": {1, 2, 4}, "SoftmaxEnd": {1, 2, 4}, "GradientEnd": {1, 2, 4}}, tiles
     assert joins == {False, True} and pieces == {1, 2} and ragged == {"StatsEnd0", "StatsEnd1", "SoftmaxEnd0", "SoftmaxEnd1"}, (joins, pieces, ragged)
-    tiles, whole, halves, twofold, joins = {}, set(), set(), set(), set()
+    tiles, whole, slices, halves, joins, short = {}, set(), set(), set(), set(), set()
     for rows, cols in gpu_orthogonal.SHAPES + gpu_orthogonal.LARGE:
         for call, how in ((c.orthogonalize, {"odt": BF16}), (c.orthogonalize, {"odt": F32}), (c.step, {})):
             got = [kind(s) for s in c.of(call, 1, rows, cols, **how)]
             grids = [t[0] for t in call(1, rows, cols, **how)[1]]
             for (name, ends, numbers), grid in zip(got, grids):
-                if name == "whole_kernel":
-                    whole.add(numbers[0])
+                if name in ("whole_kernel", "slice_kernel"):
+                    (whole if name == "whole_kernel" else slices).add(numbers[0])
                 elif name == "tiles_kernel":
                     tiles.setdefault(ends[0], set()).add(numbers[-1])
                     side = -(-min(rows, cols) // (64 * numbers[-1]))
                     if ends[0] != "UpdateEnd" and side > 1:
                         halves.add(grid < side * side)
             joins.add(any(name == "join_kernel" for name, _, _ in got))
-    assert whole == {32, 64, 96, 128} and halves == {False, True} and joins == {False, True}, (whole, halves, joins)
+            if min(rows, cols) <= 128 and max(rows, cols) > 320:
+                short.add(any(name == "slice_kernel" for name, _, _ in got))
+    assert whole == slices == {32, 64, 96, 128} and short == {True, False} and halves == {False, True} and joins == {False, True}, (whole, slices, short, halves, joins)
     assert all(t >= {1, 2} for t in tiles.values()) and len(tiles) == 3, tiles
-    shorter = [min(s) for s in gpu_orthogonal.SHAPES + gpu_orthogonal.LARGE if max(s) > 512]
+    shorter = [min(s) for s in gpu_orthogonal.SHAPES + gpu_orthogonal.LARGE if min(s) > 128]
     assert any(s < 256 for s in shorter) and any(256 <= s < 512 for s in shorter) and any(512 <= s < 1024 for s in shorter) and any(s >= 1024 for s in shorter)
 
 
