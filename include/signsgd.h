@@ -471,6 +471,7 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
 #define SS_LOSS_MAX_ROWS ((size_t)1 << 24)
 #define SS_LOSS_MAX_VOCAB ((size_t)1 << 24)
 #define SS_LOSS_MAX_WIDTH ((size_t)1 << 20)
+#define SS_LOSS_MAX_ELEMENTS ((size_t)1 << 34)      /* of h, with T and K rounded up to 64 */
 size_t ss_cross_entropy_scratch_bytes(size_t T, size_t V, size_t K);
 
 /*
@@ -506,7 +507,7 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
  * (transposed where g has more rows than columns; five steps bring every singular value above 0.01 of the
  * norm to between 0.68 and 1.2).  A matrix of zeros gives zeros; one with an infinity or a NaN, NaN everywhere.
  * The scale of g makes no difference.  Products take operands of 11 bits, X is held in 22 and sums in fp32: five steps are off by
- * 1e-3 to 2e-3 of the result's norm, which is what rounding it to bf16 costs.
+ * 1e-3 to 2e-3 of the result's norm, which is what rounding it to bf16 costs; further steps enlarge that.
  *   count, rows, cols   a stack of matrices, each by itself; any may be 0
  *   ld, apart           elements from one row to the next, and from one matrix to the next
  *   scratch             ss_orthogonalize_scratch_bytes(count, rows, cols) bytes, under the same terms

@@ -21,7 +21,9 @@ inline Span matrix(const void *p, size_t rows, size_t cols, size_t ld, ss_dtype 
     return span(p, rows && cols ? ((rows - 1) * ld + cols) * grad_bytes(dt) : 0, written);
 }
 
-inline bool bad_sizes(size_t T, size_t V, size_t K) { return T > SS_LOSS_MAX_ROWS || V > SS_LOSS_MAX_VOCAB || K == 0 || K > SS_LOSS_MAX_WIDTH || V == 0; }
+inline bool bad_sizes(size_t T, size_t V, size_t K) {
+    return T > SS_LOSS_MAX_ROWS || V > SS_LOSS_MAX_VOCAB || K == 0 || K > SS_LOSS_MAX_WIDTH || V == 0 || rounded(T, 64) * rounded(K, 64) > SS_LOSS_MAX_ELEMENTS;
+}
 inline bool bad_ld(size_t ld, size_t cols) { return ld < cols || ld > 2 * SS_LOSS_MAX_WIDTH; }
 
 // Whether the products load the caller's matrix as it lies.  Rows at multiples of 16 bytes are; a load of 16 bytes also goes to multiples of 4, but takes longer, which many rows of h

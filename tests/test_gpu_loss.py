@@ -90,6 +90,40 @@ def test_large_sizes(T, V, K):
     check(got, plain.softmax_loss(h, w, target, dloss), (target >= 0).cpu())
 
 
+@pytest.mark.parametrize("K", [1152, 1151])
+def test_weights_beyond_4_gib(K):
+    """and the gradients' rows at their end, which tiles find at offsets of more than 32 bits; read in place, and copied"""
+    T, V = 3, 1_900_003
+    gen = torch.Generator(device=DEV).manual_seed(K)
+    w = torch.empty(V, K, dtype=torch.bfloat16, device=DEV).normal_(0, K ** -0.5, generator=gen)
+    h = torch.randn(T, K, generator=gen, device=DEV).bfloat16()
+    target, dloss = torch.tensor([V - 1, -1, 7], device=DEV), torch.tensor([1.0, 5.0, -0.5], device=DEV)
+    assert w.numel() * 2 > 1 << 32
+    dw = torch.full_like(w, NAN)
+    loss, lse, dh, scratch = torch.empty(T, device=DEV), torch.empty(T, device=DEV), torch.empty_like(h), scratch_for(T, V, K)
+    ss.cross_entropy(h, w, target, loss, lse, scratch)
+    ss.cross_entropy_grad(h, w, target, lse, dloss, dh, dw, scratch)
+    # in bands, by the same formulas
+    h64 = h.double()
+    z = torch.cat([band.double() @ h64.t() for band in w.split(1 << 17)]).t()
+    want = torch.logsumexp(z, 1)
+    ez = 2 * plain.U32 * K * float(h64.abs().amax() * w.abs().amax()) * K
+    assert ((lse.double() - want).abs() <= ez + 2 * plain.U32 * (V / 32 + 100)).all()
+    assert ((loss.double() - (want - z.gather(1, target.clamp(min=0)[:, None])[:, 0])).abs() <= 2 * ez + 2 * plain.U32 * (V / 32 + 200))[[0, 2]].all() and loss[1] == 0
+    d = (z - want[:, None]).exp()
+    d[[0, 2], target[[0, 2]]] -= 1
+    d *= torch.where(target >= 0, dloss, 0.0).double()[:, None]
+    size = 2 * plain.U16 + 2 * ez + 2 * plain.U32 * (V / 32 + 300)      # D's rounding, the result's, and what z and lse are off by, relative to the terms
+    for at in (0, V // 2, V - 1000):
+        part = d[:, at:at + 1000]
+        off = (dw[at:at + 1000].double() - part.t() @ h64).abs()
+        assert (off <= size * (part.abs().t() @ h64.abs()) + 1e-30).all(), at
+    assert torch.isfinite(dw.amax()) and torch.isfinite(dw.amin())
+    terms = sum(part.abs() @ band.double().abs() for part, band in zip(d.split(1 << 17, 1), w.split(1 << 17)))
+    value = sum(part @ band.double() for part, band in zip(d.split(1 << 17, 1), w.split(1 << 17)))
+    assert ((dh.double() - value).abs() <= size * terms + 1e-30).all() and (dh[1] == 0).all()
+
+
 @pytest.mark.parametrize("dh_type", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("dw_type", [torch.float32, torch.bfloat16])
 def test_types_of_gradients(dh_type, dw_type):

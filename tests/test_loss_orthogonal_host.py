@@ -75,9 +75,9 @@ def check_the_loss_is_refused(c):
         assert call(5, 6, 100)[0] == OK and call(5, 6, 64)[0] == OK
         assert call(5, 6, 100, dt=F32) == (DTYPE, []) and call(5, 6, 100, dt=2) == (DTYPE, [])
         assert call(5, 0, 100, scratch=good, bytes=1 << 20) == (ARG, []) and call(5, 6, 0, scratch=good, bytes=1 << 20) == (ARG, [])
-        for sizes in (((1 << 24) + 1, 6, 8), (5, (1 << 24) + 1, 8), (5, 6, (1 << 20) + 1), ((1 << 64) - 1, 6, 8), (5, (1 << 64) - 1, 8)):
+        for sizes in (((1 << 24) + 1, 6, 8), (1 << 24, 6, 1100), (5, (1 << 24) + 1, 8), (5, 6, (1 << 20) + 1), ((1 << 64) - 1, 6, 8), (5, (1 << 64) - 1, 8)):
             at = {k: good for k in ("h", "w", "target", "loss", "lse", "dloss", "dh", "dw")}
-            assert call(*sizes, ldh=8, ldw=8, **at) == (ARG, []), sizes
+            assert call(*sizes, ldh=max(8, min(sizes[2], 1 << 20)), ldw=max(8, min(sizes[2], 1 << 20)), **at) == (ARG, []), sizes
         assert call(5, 6, 100, ldh=99) == (ARG, []) and call(5, 6, 100, ldw=99) == (ARG, []) and call(5, 6, 100, ldh=1 << 22, h=good) == (ARG, [])
         for name in ("h", "w", "target", "lse"):
             assert call(5, 6, 100, **{name: 0}) == (NULL, []), name
