@@ -197,16 +197,20 @@ __device__ __forceinline__ void store_out(void *to, bool bf16, size_t at, const 
 }
 
 // What becomes of eight neighbouring sums, as an End says it: load() brings what it takes besides (None where that is nothing), finish() computes, put() writes.  kStrips: it is given
-// them so, and not a wave's whole tile; kParts: the sum over k may come in parts; kSymmetric: the result may be computed by half; kRagged: b's last step along k is not whole.
+// them so, and not a wave's whole tile; kParts: the sum over k may come in parts; kSymmetric: the result may be computed by half; kRagged: b's last step along k is not whole; kShort: both operands down k may be
+// of one step.
 struct None {};
 
 // Tiles of 2 x 2 waves, each 32 T rows by 32 T columns of the result.  A step is 64 of k, multiplied in four quarters; the fragments of the
 // next quarter are read while one is multiplied.  Operands are loaded straight into LDS, which has room for five operands' steps: both of the one that is
 // read, both of the next one and the first of the one after that.  So there is always something to load: the second operand of the next step right after the last one's
 // place is free, then the first one of the step after it, spread over the multiplications.
-template <typename E, bool A_DOWN, bool B_DOWN, int T, typename End>
+// SHORT: one step is all there is, and its operands all that LDS holds, so that eight blocks instead of four share a compute unit: what bounds such products is writing the result.  us, a gradient of
+// 19840 x 2258 / 84096 x 212 from 64 rows: 25.8 / 14.8, in tiles of 128 41.2 / 23.5, of 64 43.5 / 23.5.
+template <typename E, bool A_DOWN, bool B_DOWN, int T, typename End, bool SHORT = false>
 __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename End::Args> p) {
-    constexpr uint32_t B = 64 * T, kUnit = B * 128, kRing = 5 * kUnit;
+    constexpr uint32_t B = 64 * T, kUnit = B * 128, kRing = (SHORT ? 2 : 5) * kUnit;
+    static_assert(!SHORT || (T == 1 && !End::kRagged), "one strip, no mask");
     constexpr int L = 2 * T;
     __shared__ __attribute__((aligned(1024))) char lds[kRing];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
@@ -259,7 +263,22 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
     if constexpr (End::kRagged)
 #pragma unroll
         for (int j = 0; j < 4; ++j) kept[j] = u32x4{~0u, ~0u, ~0u, ~0u};
-    if (from < to) {
+    if constexpr (SHORT) {
+#pragma unroll
+        for (int i = 0; i < L; ++i) wa.fetch(lds, i, 0, 0, 0, wave), wb.fetch(lds, i, kUnit, 0, 0, wave);
+        arrived<0>();
+        __builtin_amdgcn_s_barrier();
+        Fragments<T> f[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < 2 * T; ++i) read(f[j], i, j, 0, kUnit);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int part = 0; part < 2 * T; ++part) multiply<E>(c, f[j], part);
+        arrived<0>();       // what was read is here before the strips take its place
+    } else if (from < to) {
         Fragments<T> f0, f1;
         uint32_t a = 0, b = kUnit, a1 = 2 * kUnit, b1 = 3 * kUnit, free = 4 * kUnit;     // places of this step's operands, the next one's, and of what comes next
 #pragma unroll
@@ -332,7 +351,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
         // The result passes through LDS, 32 rows of a wave at a time, so that a lane has eight neighbours of a row and stores take whole lines.  Each wave has a part of
         // the ring to itself; chunk c (four sums) of row r lies at place c ^ r, for the banks' sake.
         constexpr uint32_t kChunks = 8 * T, kStrip = 32 * kChunks * 16, kAcross = 4 * T, kRows = 64 / kAcross;
-        char *mine = lds + wave * 2 * kStrip;
+        char *mine = lds + wave * (SHORT ? 1 : 2) * kStrip;
         __builtin_amdgcn_s_barrier();       // all have read what the ring held
         const uint32_t of = lane / kAcross, eight = lane % kAcross, col = n0 + nb + eight * 8;
 #pragma unroll

@@ -75,6 +75,13 @@ struct Product {
 
 template <typename E, bool A_DOWN, bool B_DOWN, typename End>
 int run(const Plan &plan, const Product &p, const typename End::Args &end, hipStream_t stream) {
+    if constexpr (End::kShort && A_DOWN && B_DOWN) {
+        const size_t short_m = tiles_of(p.M, 1), short_n = tiles_of(p.N, 1), blocks = short_m * short_n * p.count;
+        if (p.steps == 1 && blocks <= kMaxBlocks) {
+            const TilesArgs<typename End::Args> args{p.a, p.b, (uint32_t)p.M, (uint32_t)p.N, 1, kStep, 1, (uint32_t)short_m, (uint32_t)short_n, 1, 0, nullptr, end};
+            return host::launch(tiles_kernel<E, A_DOWN, B_DOWN, 1, End, true>, blocks, 0, stream, args, 256);
+        }
+    }
     const size_t tiles_m = tiles_of(p.M, plan.tile), tiles_n = tiles_of(p.N, plan.tile), bands = plan.half ? bands_of(tiles_m) : 0;
     const size_t blocks = (bands ? half_tiles((uint32_t)tiles_m, (uint32_t)bands) : tiles_m * tiles_n) * plan.splits * p.count;
     if (blocks > kMaxBlocks) return SS_ERR_ARG;

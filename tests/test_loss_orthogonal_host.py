@@ -166,17 +166,17 @@ def check_every_kernel_is_reached(c):
 
 def check_gpu_tests_reach_both_sides(c):
     sizes, tiles, joins = gpu_loss.SIZES + gpu_loss.LARGE, {}, set()
-    pieces, ragged = set(), set()
+    pieces, ragged, once = set(), set(), set()
     for T, V, K in sizes:
         got = [kind(s) for call in (c.loss, c.grad) for s in c.of(call, T, V, K)]
         for name, ends, numbers in got:
             if name == "tiles_kernel":
                 tiles.setdefault(ends[0], set()).add(numbers[2])
-                ragged.update({ends[0] + str(numbers[3])} if len(numbers) > 3 else ())
+                (once if ends[0] == "GradientEnd" else ragged).add(ends[0] + str(numbers[3]))
         joins.add(any(name == "join_kernel" for name, _, _ in got))
         pieces.add(min(2, sum(ends == ["SoftmaxEnd"] for _, ends, _ in got)))
     assert tiles == {"StatsEnd": {1, 2, 4}, "SoftmaxEnd": {1, 2, 4}, "GradientEnd": {1, 2, 4}}, tiles
-    assert joins == {False, True} and pieces == {1, 2} and ragged == {"StatsEnd0", "StatsEnd1", "SoftmaxEnd0", "SoftmaxEnd1"}, (joins, pieces, ragged)
+    assert joins == {False, True} and pieces == {1, 2} and ragged == {"StatsEnd0", "StatsEnd1", "SoftmaxEnd0", "SoftmaxEnd1"} and len(once) == 2, (joins, pieces, ragged, once)
     tiles, whole, slices, halves, joins, short = {}, set(), set(), set(), set(), set()
     for rows, cols in gpu_orthogonal.SHAPES + gpu_orthogonal.LARGE:
         for call, how in ((c.orthogonalize, {"odt": BF16}), (c.orthogonalize, {"odt": F32}), (c.step, {})):
@@ -186,8 +186,8 @@ def check_gpu_tests_reach_both_sides(c):
                 if name in ("whole_kernel", "slice_kernel"):
                     (whole if name == "whole_kernel" else slices).add(numbers[0])
                 elif name == "tiles_kernel":
-                    tiles.setdefault(ends[0], set()).add(numbers[-1])
-                    side = -(-min(rows, cols) // (64 * numbers[-1]))
+                    tiles.setdefault(ends[0], set()).add(numbers[2])
+                    side = -(-min(rows, cols) // (64 * numbers[2]))
                     if ends[0] != "UpdateEnd" and side > 1:
                         halves.add(grid < side * side)
             joins.add(any(name == "join_kernel" for name, _, _ in got))
