@@ -71,7 +71,7 @@ struct ForwardPlace {
             size_t count = 0;
             for (size_t v = 0; v < s.V; v += s.forward(copy)) {
                 const size_t n = std::min(s.forward(copy), s.V - v);
-                count += 2 * tiles_of(n, product::plan_of(s.T, n, s.K64, 1, false).tile);
+                count += 2 * tiles_of(n, product::plan_of(s.T, n, s.K64, 1, false, false, false).tile);
             }
             most = std::max(most, count);
         }
@@ -167,7 +167,7 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
         rc = prepare(before, stream);
         if (rc != SS_OK) return rc;
         before = {};
-        const Plan plan = product::plan_of(T, n, s.K64, 1, false);
+        const Plan plan = product::plan_of(T, n, s.K64, 1, false, false, false);
         const Operand ws = copy ? rows_of(from, n, s.K64, s.K64, n, 0) : rows_of(from, n, K, ldw, n, 0);
         rc = along_weights<loss::StatsEnd>(plan, {rows_of(h, T, s.K64, ldh, T, 0), ws, 1, T, n, s.K64 / product::kStep, nullptr}, K, copy,
                                            {parts, picked, target, (int64_t)v, (uint32_t)count}, stream);

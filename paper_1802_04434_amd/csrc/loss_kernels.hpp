@@ -26,7 +26,7 @@ struct Part {
 
 template <bool RAGGED>
 struct StatsEnd {
-    static constexpr bool kStrips = false, kShort = false, kParts = false, kRagged = RAGGED;
+    static constexpr bool kStrips = false, kParts = false, kRagged = RAGGED;
     struct Args {
         Part *parts;               // (half a tile's columns, row)
         float *picked;             // the target's logit, by row
@@ -178,7 +178,7 @@ __device__ __forceinline__ void write_factors(const FactorArgs &a) {
 // D, whole eights of columns and rows: zero beyond the vocabulary and in rows without a target
 template <bool RAGGED>
 struct SoftmaxEnd {
-    static constexpr bool kStrips = true, kShort = false, kParts = false, kSymmetric = false, kRagged = RAGGED;
+    static constexpr bool kStrips = true, kParts = false, kSymmetric = false, kRagged = RAGGED;
     struct Args {
         const float *lse, *factor;
         const int64_t *target;
@@ -216,7 +216,7 @@ struct SoftmaxEnd {
 
 // A gradient, or with the pieces before it the sum so far
 struct GradientEnd {
-    static constexpr bool kStrips = true, kShort = true, kParts = true, kSymmetric = false, kRagged = false;
+    static constexpr bool kStrips = true, kParts = true, kSymmetric = false, kRagged = false;
     struct Args {
         const float *scale;
         float *sum;                // rows x N: not wanted where a piece is all there is

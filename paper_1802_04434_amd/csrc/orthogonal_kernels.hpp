@@ -174,7 +174,7 @@ __device__ __forceinline__ void sum_halves(f32x4 (&v)[2], const Eight &e) {
 
 // A = X X', from sums that are scaled twice
 struct SquareEnd {
-    static constexpr bool kStrips = true, kShort = false, kParts = true, kSymmetric = true, kRagged = false;
+    static constexpr bool kStrips = true, kParts = true, kSymmetric = true, kRagged = false;
     struct Args {
         _Float16 *hi, *lo;
         uint64_t apart;
@@ -192,7 +192,7 @@ struct SquareEnd {
 
 // B + mu I = b A + c A A + mu I
 struct PolynomialEnd {
-    static constexpr bool kStrips = true, kShort = false, kParts = false, kSymmetric = true, kRagged = false;
+    static constexpr bool kStrips = true, kParts = false, kSymmetric = true, kRagged = false;
     struct Args {
         const _Float16 *a_hi, *a_lo;
         _Float16 *hi, *lo;
@@ -219,7 +219,7 @@ struct PolynomialEnd {
 
 // X <- (a - mu) X + (B + mu I) X; the last time into the result, or off the parameters
 struct UpdateEnd {
-    static constexpr bool kStrips = true, kShort = false, kParts = false, kSymmetric = false, kRagged = false;
+    static constexpr bool kStrips = true, kParts = false, kSymmetric = false, kRagged = false;
     struct Args {
         const _Float16 *hi, *lo;
         _Float16 *hi_out, *lo_out;

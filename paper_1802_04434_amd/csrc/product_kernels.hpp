@@ -197,20 +197,20 @@ __device__ __forceinline__ void store_out(void *to, bool bf16, size_t at, const 
 }
 
 // What becomes of eight neighbouring sums, as an End says it: load() brings what it takes besides (None where that is nothing), finish() computes, put() writes.  kStrips: it is given
-// them so, and not a wave's whole tile; kParts: the sum over k may come in parts; kSymmetric: the result may be computed by half; kRagged: b's last step along k is not whole; kShort: both operands down k may be
-// of one step.
+// them so, and not a wave's whole tile; kParts: the sum over k may come in parts; kSymmetric: the result may be computed by half; kRagged: b's last step along k is not whole.
 struct None {};
 
 // Tiles of 2 x 2 waves, each 32 T rows by 32 T columns of the result.  A step is 64 of k, multiplied in four quarters; the fragments of the
 // next quarter are read while one is multiplied.  Operands are loaded straight into LDS, which has room for five operands' steps: both of the one that is
 // read, both of the next one and the first of the one after that.  So there is always something to load: the second operand of the next step right after the last one's
 // place is free, then the first one of the step after it, spread over the multiplications.
-// SHORT: one step is all there is, and its operands all that LDS holds, so that eight blocks instead of four share a compute unit: what bounds such products is writing the result.  us, a gradient of
-// 19840 x 2258 / 84096 x 212 from 64 rows: 25.8 / 14.8, in tiles of 128 41.2 / 23.5, of 64 43.5 / 23.5.
+// SHORT, for a few steps: one step is all that LDS holds, so that eight blocks instead of four share a compute unit, and wait for their loads and write their results in turn: that is what bounds such
+// products.  us, SHORT / tiles of 64 / of 128: gradients of 19840 x 2258 from 64 rows 25.9 / 43.5 / 41.0, 84096 x 212 from 64 15.2 / 23.5 / 24.2, 32000 x 1024 from 128 23.8 / 38.9 / 32.1, 32000 x 2048 from 256
+// 57.3 / 89.3 / 69.7, 32000 x 512 from 512 28.6 / - / 26.5.
 template <typename E, bool A_DOWN, bool B_DOWN, int T, typename End, bool SHORT = false>
 __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename End::Args> p) {
     constexpr uint32_t B = 64 * T, kUnit = B * 128, kRing = (SHORT ? 2 : 5) * kUnit;
-    static_assert(!SHORT || (T == 1 && !End::kRagged), "one strip, no mask");
+    static_assert(!SHORT || T == 1, "one strip");
     constexpr int L = 2 * T;
     __shared__ __attribute__((aligned(1024))) char lds[kRing];
     const uint32_t lane = threadIdx.x & 63u, wave = uniform(threadIdx.x >> 6);
@@ -260,23 +260,42 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
 #pragma unroll
             for (int i = 0; i < T; ++i) f.b[i] &= kept[j];
     };
+    auto mask = [&] {
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+            for (uint32_t d = 0; d < 4; ++d) {
+                const uint32_t k = 32 * q + 8 * j + 2 * d;
+                kept[j][d] = k + 1 < p.tail ? ~0u : k < p.tail ? 0xFFFFu : 0u;
+            }
+    };
     if constexpr (End::kRagged)
 #pragma unroll
         for (int j = 0; j < 4; ++j) kept[j] = u32x4{~0u, ~0u, ~0u, ~0u};
     if constexpr (SHORT) {
+        for (uint32_t step = 0; step < p.steps; ++step) {
+            if (step) __builtin_amdgcn_s_barrier();     // all have read the one before it
+            const At coming = step_of(step);
 #pragma unroll
-        for (int i = 0; i < L; ++i) wa.fetch(lds, i, 0, 0, 0, wave), wb.fetch(lds, i, kUnit, 0, 0, wave);
-        arrived<0>();
-        __builtin_amdgcn_s_barrier();
-        Fragments<T> f[4];
+            for (int i = 0; i < L; ++i) wa.fetch(lds, i, 0, coming.step, coming.a, wave), wb.fetch(lds, i, kUnit, coming.step, coming.b, wave);
+            arrived<0>();
+            __builtin_amdgcn_s_barrier();
+            Fragments<T> f[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < 2 * T; ++i) read(f[j], i, j, 0, kUnit);
+                for (int i = 0; i < 2 * T; ++i) read(f[j], i, j, 0, kUnit);
+            if constexpr (End::kRagged) {
+                if (step + 1 == to) mask();
+            }
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j) {
+                keep(f[j], j);
 #pragma unroll
-            for (int part = 0; part < 2 * T; ++part) multiply<E>(c, f[j], part);
+                for (int part = 0; part < 2 * T; ++part) multiply<E>(c, f[j], part);
+            }
+            arrived<0>();
+        }
         arrived<0>();       // what was read is here before the strips take its place
     } else if (from < to) {
         Fragments<T> f0, f1;
@@ -295,14 +314,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
         for (uint32_t step = from; step < to; ++step) {
             const At coming = step_of(step + 2);
             if constexpr (End::kRagged) {
-                if (step + 1 == to)
-#pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j)
-#pragma unroll
-                        for (uint32_t d = 0; d < 4; ++d) {
-                            const uint32_t k = 32 * q + 8 * j + 2 * d;
-                            kept[j][d] = k + 1 < p.tail ? ~0u : k < p.tail ? 0xFFFFu : 0u;
-                        }
+                if (step + 1 == to) mask();
             }
             keep(f0, 0);
             // Part by part, with a read and perhaps a load in each: in one go they would keep the matrix unit waiting while their queues are full

@@ -17,6 +17,7 @@ struct Plan {
     int tile;
     size_t splits;
     bool half = false;
+    bool few = false;          // steps, so few that a block holds one at a time
 };
 
 inline size_t bands_of(size_t tiles) { return (tiles + kHigh - 1) / kHigh; }
@@ -44,7 +45,11 @@ inline double cost_of(size_t M, size_t N, size_t K, size_t count, const Plan &pl
     return us;
 }
 
-inline Plan plan_of(size_t M, size_t N, size_t K, size_t count, bool may_split, bool symmetric = false) {
+// Up to four steps, where more blocks than four a compute unit write their results (a softmax's statistics are little to write), a block holds one step at a time.  us, so / otherwise: gradients of 8192 rows against
+// 128000 x 256 2,578 / 2,784, 128000 x 64 1,741 / 1,996, 48 of 250 x 700 orthogonalised 199 / 247; but a loss of 4096 rows against 32000 x 256 156 / 124, one matrix of 256 x 256 91 / 84.
+constexpr size_t kFewSteps = 4, kFewBlocks = 1024;
+
+inline Plan plan_of(size_t M, size_t N, size_t K, size_t count, bool may_split, bool symmetric = false, bool written = true) {
     const size_t steps = (K + kStep - 1) / kStep;
     Plan best{1, 1};
     double least = 1e300;
@@ -52,6 +57,8 @@ inline Plan plan_of(size_t M, size_t N, size_t K, size_t count, bool may_split, 
         const double us = cost_of(M, N, K, count, plan);
         if (us < least) least = us, best = plan;
     };
+    const size_t small = tiles_of(M, 1) * tiles_of(N, 1) * count;
+    if (written && small <= kMaxBlocks && (steps == 1 || (steps <= kFewSteps && small > kFewBlocks))) return {1, 1, false, true};
     for (const Shape &s : kShapes) {
         const size_t tiles = tiles_of(M, s.tile) * tiles_of(N, s.tile) * count;
         consider({s.tile, 1});
@@ -75,18 +82,14 @@ struct Product {
 
 template <typename E, bool A_DOWN, bool B_DOWN, typename End>
 int run(const Plan &plan, const Product &p, const typename End::Args &end, hipStream_t stream) {
-    if constexpr (End::kShort && A_DOWN && B_DOWN) {
-        const size_t short_m = tiles_of(p.M, 1), short_n = tiles_of(p.N, 1), blocks = short_m * short_n * p.count;
-        if (p.steps == 1 && blocks <= kMaxBlocks) {
-            const TilesArgs<typename End::Args> args{p.a, p.b, (uint32_t)p.M, (uint32_t)p.N, 1, kStep, 1, (uint32_t)short_m, (uint32_t)short_n, 1, 0, nullptr, end};
-            return host::launch(tiles_kernel<E, A_DOWN, B_DOWN, 1, End, true>, blocks, 0, stream, args, 256);
-        }
-    }
     const size_t tiles_m = tiles_of(p.M, plan.tile), tiles_n = tiles_of(p.N, plan.tile), bands = plan.half ? bands_of(tiles_m) : 0;
     const size_t blocks = (bands ? half_tiles((uint32_t)tiles_m, (uint32_t)bands) : tiles_m * tiles_n) * plan.splits * p.count;
     if (blocks > kMaxBlocks) return SS_ERR_ARG;
     const TilesArgs<typename End::Args> args{p.a, p.b, (uint32_t)p.M, (uint32_t)p.N, (uint32_t)(p.twofold ? 3 * p.steps : p.steps), (uint32_t)p.tail, (uint32_t)p.steps, (uint32_t)tiles_m, (uint32_t)tiles_n, (uint32_t)plan.splits, (uint32_t)bands, p.parts, end};
-    const auto kernel = plan.tile == 4 ? tiles_kernel<E, A_DOWN, B_DOWN, 4, End> : plan.tile == 2 ? tiles_kernel<E, A_DOWN, B_DOWN, 2, End> : tiles_kernel<E, A_DOWN, B_DOWN, 1, End>;
+    const auto kernel = plan.few         ? tiles_kernel<E, A_DOWN, B_DOWN, 1, End, End::kStrips>
+                        : plan.tile == 4 ? tiles_kernel<E, A_DOWN, B_DOWN, 4, End>
+                        : plan.tile == 2 ? tiles_kernel<E, A_DOWN, B_DOWN, 2, End>
+                                         : tiles_kernel<E, A_DOWN, B_DOWN, 1, End>;
     const int rc = host::launch(kernel, blocks, 0, stream, args, 256);
     if (rc != SS_OK || plan.splits == 1) return rc;
     if constexpr (End::kParts) {

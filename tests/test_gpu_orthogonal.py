@@ -84,6 +84,19 @@ def test_large_matrices(rows, cols):
     assert off <= bound + 3 * plain.U32 * float(want.norm() + p.numel() ** 0.5), (off, bound)
 
 
+@pytest.mark.parametrize("count,rows,cols", [(300, 150, 250), (300, 250, 150), (700, 60, 70), (40, 30, 500), (17, 500, 120)])
+def test_many_matrices(count, rows, cols):
+    """stacks that fill the card several times: each as if it were alone"""
+    gen = torch.Generator(device=DEV).manual_seed(count)
+    x = torch.randn(count, rows, cols, generator=gen, device=DEV)
+    out = torch.empty(count, rows, cols, device=DEV)
+    ss.orthogonalize(x, out, scratch_for(rows, cols, count))
+    for i in (0, 1, count // 2, count - 1):
+        want = plain.orthogonalized(x[i])
+        off = float((out[i].double() - want).norm())
+        assert off <= plain.orthogonal_bound(x[i]) + plain.U32 * float(want.norm()), (i, off)
+
+
 @pytest.mark.parametrize("kind", ["normal", "singular"])
 @pytest.mark.parametrize("rows,cols", [(64, 64), (130, 200), (300, 150)])
 def test_other_spectra(rows, cols, kind):

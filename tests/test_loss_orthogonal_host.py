@@ -146,7 +146,7 @@ def kind(symbol):
 
 # what each kind of call meets: more than the GPU tests', for the sizes that these would take long with
 LARGE_LOSSES = [(8192, 128000, 4096), (8192, 128000, 4008), (900, 20000, 1002), (8192, 8192, 8192), (4096, 32000, 2048), (2048, 2048, 2048), (300, 700, 192), (4096, 4096, 64), (64, 64, 64), (16, 256, 8192), (1024, 1024, 8192)]
-LARGE_MATRICES = [(1, 8192, 8192), (1, 4096, 4096), (1, 2048, 2048), (1, 1024, 1024), (1, 512, 4096), (1, 4096, 512), (24, 512, 2048), (24, 2048, 512), (1, 20, 30), (1, 30, 800), (1, 90, 90), (1, 250, 80), (1, 100, 30), (1, 60, 300), (1, 130, 8192), (1, 128, 100_000), (1, 100_000, 128), (1, 8192, 130), (8, 4096, 8192),
+LARGE_MATRICES = [(1, 8192, 8192), (1, 4096, 4096), (1, 2048, 2048), (1, 1024, 1024), (1, 512, 4096), (1, 4096, 512), (24, 512, 2048), (24, 2048, 512), (1, 20, 30), (1, 30, 800), (1, 90, 90), (1, 250, 80), (1, 100, 30), (1, 60, 300), (1, 130, 8192), (1, 128, 100_000), (1, 100_000, 128), (300, 150, 250), (300, 250, 150), (1, 8192, 130), (8, 4096, 8192),
                   (8, 8192, 4096), (1, 32768, 2048), (1, 2048, 32768)]
 
 
@@ -166,18 +166,19 @@ def check_every_kernel_is_reached(c):
 
 def check_gpu_tests_reach_both_sides(c):
     sizes, tiles, joins = gpu_loss.SIZES + gpu_loss.LARGE, {}, set()
-    pieces, ragged, once = set(), set(), set()
+    pieces, ragged, few = set(), set(), set()
     for T, V, K in sizes:
         got = [kind(s) for call in (c.loss, c.grad) for s in c.of(call, T, V, K)]
         for name, ends, numbers in got:
             if name == "tiles_kernel":
                 tiles.setdefault(ends[0], set()).add(numbers[2])
-                (once if ends[0] == "GradientEnd" else ragged).add(ends[0] + str(numbers[3]))
+                few.add(ends[0] + str(numbers[-1]))
+                ragged.update({ends[0] + str(numbers[3])} if len(numbers) > 4 else ())
         joins.add(any(name == "join_kernel" for name, _, _ in got))
         pieces.add(min(2, sum(ends == ["SoftmaxEnd"] for _, ends, _ in got)))
     assert tiles == {"StatsEnd": {1, 2, 4}, "SoftmaxEnd": {1, 2, 4}, "GradientEnd": {1, 2, 4}}, tiles
-    assert joins == {False, True} and pieces == {1, 2} and ragged == {"StatsEnd0", "StatsEnd1", "SoftmaxEnd0", "SoftmaxEnd1"} and len(once) == 2, (joins, pieces, ragged, once)
-    tiles, whole, slices, halves, joins, short = {}, set(), set(), set(), set(), set()
+    assert joins == {False, True} and pieces == {1, 2} and ragged == {"StatsEnd0", "StatsEnd1", "SoftmaxEnd0", "SoftmaxEnd1"} and few == {"StatsEnd0", "SoftmaxEnd0", "SoftmaxEnd1", "GradientEnd0", "GradientEnd1"}, (joins, pieces, ragged, few)
+    tiles, whole, slices, halves, joins, short, few = {}, set(), set(), set(), set(), set(), set()
     for rows, cols in gpu_orthogonal.SHAPES + gpu_orthogonal.LARGE:
         for call, how in ((c.orthogonalize, {"odt": BF16}), (c.orthogonalize, {"odt": F32}), (c.step, {})):
             got = [kind(s) for s in c.of(call, 1, rows, cols, **how)]
@@ -187,12 +188,14 @@ def check_gpu_tests_reach_both_sides(c):
                     (whole if name == "whole_kernel" else slices).add(numbers[0])
                 elif name == "tiles_kernel":
                     tiles.setdefault(ends[0], set()).add(numbers[2])
+                    few.add(numbers[-1])
                     side = -(-min(rows, cols) // (64 * numbers[2]))
                     if ends[0] != "UpdateEnd" and side > 1:
                         halves.add(grid < side * side)
             joins.add(any(name == "join_kernel" for name, _, _ in got))
             if min(rows, cols) <= 128 and max(rows, cols) > 320:
                 short.add(any(name == "slice_kernel" for name, _, _ in got))
+    assert few == {0, 1}, few
     assert whole == slices == {32, 64, 96, 128} and short == {True, False} and halves == {False, True} and joins == {False, True}, (whole, slices, short, halves, joins)
     assert all(t >= {1, 2} for t in tiles.values()) and len(tiles) == 3, tiles
     shorter = [min(s) for s in gpu_orthogonal.SHAPES + gpu_orthogonal.LARGE if min(s) > 128]
