@@ -475,7 +475,8 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
 size_t ss_cross_entropy_scratch_bytes(size_t T, size_t V, size_t K);
 
 /*
- * lse_t <- log sum_v exp(z_tv);  loss_t <- lse_t - z_t,target_t, 0 in rows without a target.
+ * lse_t <- log sum_v exp(z_tv);  loss_t <- lse_t - z_t,target_t, 0 in rows without a target.  The loss
+ * is computed from the largest logit: a likely target's is not rounded by the size of the logits.
  *   loss, lse  out  T x fp32.  A row with an infinite or NaN logit has NaN, but one of -infinity
  *                   next to finite ones counts as zero probability.
  */

@@ -122,10 +122,12 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const JoinArgs a) {
     }
     if (threadIdx.x >= a.rows || row >= a.T) return;
     s = shared[threadIdx.x];
-    const float lse = s.top + logf(s.sum);
+    const float log_sum = logf(s.sum);
     const int64_t target = a.target[row];
-    a.lse[row] = lse;
-    a.loss[row] = target < 0 ? 0.0f : target < a.V ? lse - a.picked[row] : __builtin_nanf("");
+    a.lse[row] = s.top + log_sum;
+    // Not lse - picked: lse is rounded by the logits' size, 6e-5 where they are near 1000, while top - picked is exact wherever they are near each other, and 0 where the target is the
+    // likeliest, whose loss is then the logarithm alone.
+    a.loss[row] = target < 0 ? 0.0f : target < a.V ? (s.top - a.picked[row]) + log_sum : __builtin_nanf("");
 }
 
 // ------------------------------------------------------------ backward ----

@@ -1,0 +1,44 @@
+"""Values of the loss and its gradient that bounds over whole matrices would hide, on the GPU, on operands whose products add up exactly."""
+import pytest
+import torch
+
+import loss_plain as plain
+import paper_1802_04434_amd as ss
+from test_gpu_loss import DEV, NAN, scratch_for
+
+pytestmark = pytest.mark.gpu
+
+
+def confident(T, V, base):
+    """h, w, target and z with z[t, target[t]] = base^2, the largest of its row by 8 to 16: whole sixteenths, which bf16 and every fp32 sum hold"""
+    kinds = 7
+    gen = torch.Generator().manual_seed(T * 31 + V)
+    gap = torch.randint(128, 257, (kinds, V), generator=gen).float() / 16
+    likely = torch.randint(0, V, (kinds,), generator=gen)
+    gap[torch.arange(kinds), likely] = 0
+    kind = torch.arange(T) % kinds
+    h, w = torch.zeros(T, 1 + kinds), torch.zeros(V, 1 + kinds)
+    h[:, 0], w[:, 0], w[:, 1:] = base, base, -gap.t()
+    h[torch.arange(T), 1 + kind] = 1
+    h, w = h.bfloat16(), w.bfloat16()
+    z = h.double() @ w.double().t()
+    assert torch.equal(z, (base * base - gap.double())[kind])
+    return h, w, likely[kind], z
+
+
+@pytest.mark.parametrize("base", [32.0, 128.0])
+@pytest.mark.parametrize("T,V", [(1, 300), (40, 300), (7, 9000), (1100, 1000)])
+def test_a_confident_rows_loss_does_not_go_by_the_size_of_its_logits(T, V, base):
+    """z is exact, so that top - z[target] is 0 and the loss is log(sum of exp(z - top)), a sum of 1 and what is small.  A term e^-g is off by the rounding of g log2(e), g <= 16,
+    by half a step of each of log2(e) and the product, and by two steps of the function: (2 x 16 + 4) U32 of itself; an addition by U32 of a sum below 1 + tail, and on the way of any
+    term there are at most 128 of a lane, 2 between lanes, 8 + 1 for each group of eight parts, and 8 levels.  The logarithm of x near 1 is off by two steps of itself; lse by its rounding too."""
+    h, w, target, z = confident(T, V, base)
+    loss, lse = torch.full((T,), NAN, device=DEV), torch.full((T,), NAN, device=DEV)
+    ss.cross_entropy(h.to(DEV), w.to(DEV), target.to(DEV), loss, lse, scratch_for(T, V, h.shape[1]))
+    tail = (z - base * base).exp().sum(1) - 1
+    want = torch.log1p(tail)
+    groups = -(-V // 32 // 8) + 1           # parts of 32 columns at the least
+    off = plain.U32 * (36 * tail + (1 + tail) * (128 + 2 + 9 * groups + 8) + 4 * want)
+    assert (off < 0.4 * base * base * 2 ** -24).all() or base < 100        # a step of lse would show
+    assert ((loss.cpu().double() - want).abs() <= off).all(), float(((loss.cpu().double() - want).abs() / off).max())
+    assert ((lse.cpu().double() - (base * base + want)).abs() <= off + plain.U32 * (base * base + want)).all()
