@@ -462,7 +462,11 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
  *   scratch  work ss_cross_entropy_scratch_bytes(T, V, K) bytes of DEVICE memory, 16-byte aligned,
  *                 contents immaterial before and after; untouched by others until the enqueued work
  *                 has run (two calls that may run at the same time, or two captured graphs that may,
- *                 need two).  Smaller: SS_ERR_ARG.
+ *                 need two).  Smaller: SS_ERR_ARG.  Enough for either call at any alignment: h, dh's
+ *                 sum, partial sums, and room for half of the logits in 16 bits (of 256 MB at least, if
+ *                 there are as many, and 512 MB at most) for a piece of the softmax's gradient and of
+ *                 copied weights.  135 MB for one row against 128000 x 4096, 346 MB for 4096 against
+ *                 32000 x 2048, 730 MB for 8192 against 128000 x 4096, whose logits take 2.1 GB.
  * T may be 0; V and K may not, and none may exceed the limits below (SS_ERR_ARG).  Nothing that is written
  * may share a byte with anything else of the call.  w is read where it is if its rows are 16-byte aligned (4-byte
  * where T is small), else copied into scratch on the way, piece by piece.

@@ -48,59 +48,54 @@ int along_weights(const Plan &plan, Product p, size_t K, bool copy, const typena
     return product::run<product::Bf16, false, false, End<true>>(plan, p, __builtin_bit_cast(typename End<true>::Args, end), stream);
 }
 
-// What is computed at a time is a piece of the vocabulary.  Forward: 2^36 entries of z, or 128 MB of copied weights.  Backward: 128 MB of D, so that
-// the products that read it find it in the memory-side cache.
-constexpr size_t kPieceEntries = (size_t)1 << 28, kForwardEntries = (size_t)1 << 36, kEdge = 256;
-
-inline size_t piece_of(size_t entries, size_t rows, size_t V) { return std::min(std::max(entries / rows / kEdge * kEdge, 4 * kEdge), rounded(V, kEdge)); }
+// What is computed at a time is a piece of the vocabulary.  Forward 2^36 entries of z, of which none is kept, or as many copied weights as there is room for.  Backward there is room for half of the
+// logits in 16 bits, but for kLeastRoom entries at least and kMostRoom at most, which D shares with the copied weights; those have half of it at most.  Fewer entries cost more launches that do not
+// fill the card, and dh's fp32 sum is read and written for each piece.  us of the gradients with room for 2^26 / 2^27 / 2^28 entries: 4096 rows against 32000 x 2048 1,449 / 1,401 / 1,402, 2048 against
+// 50000 x 1024 792 / 734 / 735, 8192 against 32000 x 1024 1,704 / 1,572 / 1,532, 8192 against 128000 x 4096 20,350 / 20,241 / 19,983, with copied weights 23,480 / 21,650 / 20,930.
+constexpr size_t kForwardEntries = (size_t)1 << 36, kLeastRoom = (size_t)1 << 27, kMostRoom = (size_t)1 << 28, kEdge = 256;
 
 struct Sizes {
-    size_t T, V, K, T64, K64;
-    Sizes(size_t t, size_t v, size_t k) : T(t), V(v), K(k), T64(rounded(t, 64)), K64(rounded(k, 64)) {}
-    size_t copied() const { return piece_of(kPieceEntries, K64, V); }       // rows of weights in a copy
-    size_t forward(bool copy) const { return std::min(piece_of(kForwardEntries, T64, V), copy ? copied() : V); }
-    size_t backward(bool copy) const { return std::min(piece_of(kPieceEntries, T64, V), copy ? copied() : V); }
+    size_t T, V, K, T64, K64, room;
+    Sizes(size_t t, size_t v, size_t k) : T(t), V(v), K(k), T64(rounded(t, 64)), K64(rounded(k, 64)), room(std::min(std::max(T64 * V / 2, kLeastRoom), kMostRoom)) {}
+    // tokens of a piece, where each takes `each` entries: all pieces but the last alike, and that no shorter than it has to be
+    size_t piece(size_t entries, size_t each) const {
+        const size_t most = std::max(entries / each / kEdge * kEdge, 4 * kEdge), pieces = (V + most - 1) / most;
+        return std::min(rounded((V + pieces - 1) / pieces, kEdge), V);
+    }
+    size_t forward(bool copy) const { return std::min(piece(kForwardEntries, T64), copy ? piece(room, 2 * K64) : V); }
+    size_t backward(bool copy) const { return piece(room, copy ? std::max(T64 + K64, 2 * K64) : T64); }
+    size_t last(size_t piece) const { return V - (V - 1) / piece * piece; }
 };
 
 struct ForwardPlace {
     size_t parts, picked, h, w, bytes;
-    ForwardPlace(const Sizes &s) {
+    ForwardPlace(const Sizes &s, bool copy) {
+        const size_t piece = s.forward(copy), last = s.last(piece);
+        auto parts_of = [&](size_t n) { return 2 * tiles_of(n, product::plan_of(s.T, n, s.K64, 1, false, false, false).tile); };
         Layout l;
-        size_t most = 0;
-        for (const bool copy : {false, true}) {
-            size_t count = 0;
-            for (size_t v = 0; v < s.V; v += s.forward(copy)) {
-                const size_t n = std::min(s.forward(copy), s.V - v);
-                count += 2 * tiles_of(n, product::plan_of(s.T, n, s.K64, 1, false, false, false).tile);
-            }
-            most = std::max(most, count);
-        }
-        parts = l.take(most * s.T * sizeof(loss::Part));
+        parts = l.take(((s.V - last) / piece * parts_of(piece) + parts_of(last)) * s.T * sizeof(loss::Part));
         picked = l.take(s.T * sizeof(float));
         h = l.take(s.T64 * s.K64 * 2);
-        w = l.take(s.copied() * s.K64 * 2);
+        w = l.take(copy ? piece * s.K64 * 2 : 0);
         bytes = l.bytes;
     }
 };
 
 struct BackwardPlace {
     size_t factor, scale, h, d, w, sum, parts, bytes;
-    BackwardPlace(const Sizes &s) {
+    BackwardPlace(const Sizes &s, bool copy) {
+        const size_t piece = s.backward(copy);
         Layout l;
-        const size_t most = rounded(s.backward(false), 64);
         factor = l.take(s.T64 * sizeof(float));
         scale = l.take(sizeof(float));
         h = l.take(s.T64 * s.K64 * 2);
-        d = l.take(s.T64 * most * 2);
-        w = l.take(s.copied() * s.K64 * 2);
-        sum = l.take(s.T * s.K * sizeof(float));
+        d = l.take(s.T64 * rounded(piece, 64) * 2);
+        w = l.take(copy ? piece * s.K64 * 2 : 0);
+        sum = l.take(piece < s.V ? s.T * s.K * sizeof(float) : 0);
         size_t of_parts = 0;
-        for (const bool copy : {false, true}) {
-            const size_t piece = std::min(s.backward(copy), s.V), last = s.V - (s.V - 1) / piece * piece;
-            for (const size_t n : {piece, last}) {
-                of_parts = std::max(of_parts, parts_bytes(product::plan_of(s.T, s.K, rounded(n, 64), 1, true), 1, s.T, s.K));
-                of_parts = std::max(of_parts, parts_bytes(product::plan_of(n, s.K, s.T64, 1, true), 1, n, s.K));
-            }
+        for (const size_t n : {piece, s.last(piece)}) {
+            of_parts = std::max(of_parts, parts_bytes(product::plan_of(s.T, s.K, rounded(n, 64), 1, true), 1, s.T, s.K));
+            of_parts = std::max(of_parts, parts_bytes(product::plan_of(n, s.K, s.T64, 1, true), 1, n, s.K));
         }
         parts = l.take(of_parts);
         bytes = l.bytes;
@@ -133,7 +128,9 @@ extern "C" {
 size_t ss_cross_entropy_scratch_bytes(size_t T, size_t V, size_t K) {
     if (bad_sizes(T, V, K) || T == 0) return 0;
     const Sizes s(T, V, K);
-    return std::max(ForwardPlace(s).bytes, BackwardPlace(s).bytes);
+    size_t bytes = 0;
+    for (const bool copy : {false, true}) bytes = std::max({bytes, ForwardPlace(s, copy).bytes, BackwardPlace(s, copy).bytes});
+    return bytes;
 }
 
 int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V, size_t K, size_t ldw, const int64_t *target,
@@ -146,7 +143,8 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
                      span(scratch, scratch_bytes, true)};
     if (written_spans_overlap(spans, 6)) return SS_ERR_ARG;
     const Sizes s(T, V, K);
-    const ForwardPlace place(s);
+    const bool copy = !loadable(w, ldw, T);
+    const ForwardPlace place(s, copy);
     if (scratch_bytes < ss_cross_entropy_scratch_bytes(T, V, K)) return SS_ERR_ARG;
     char *base = static_cast<char *>(scratch);
     hipStream_t stream = static_cast<hipStream_t>(hip_stream);
@@ -155,7 +153,6 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
         before.h = copy_of(h, ldh, base + place.h, T, K, s.K64, T, nullptr);
         h = base + place.h, ldh = s.K64;
     }
-    const bool copy = !loadable(w, ldw, T);
     const size_t piece = s.forward(copy);
     loss::Part *parts = reinterpret_cast<loss::Part *>(base + place.parts);
     float *picked = reinterpret_cast<float *>(base + place.picked);
@@ -199,14 +196,14 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
         return launch(loss::zero_kernel, std::min((a.size + 255) / 256, (uint64_t)1 << 16), 0, stream, a, 256);
     }
     const Sizes s(T, V, K);
-    const BackwardPlace place(s);
+    const bool copy = !loadable(w, ldw, T);
+    const BackwardPlace place(s, copy);
     if (scratch_bytes < ss_cross_entropy_scratch_bytes(T, V, K)) return SS_ERR_ARG;
     char *base = static_cast<char *>(scratch);
     float *factor = reinterpret_cast<float *>(base + place.factor), *scale = reinterpret_cast<float *>(base + place.scale);
     float *sum = reinterpret_cast<float *>(base + place.sum), *parts = reinterpret_cast<float *>(base + place.parts);
     __bf16 *d = reinterpret_cast<__bf16 *>(base + place.d);
     loss::PrepareArgs before = {{dloss, target, factor, scale, (int64_t)V, (uint32_t)T, (uint32_t)s.T64}, copy_of(h, ldh, base + place.h, T, K, s.K64, s.T64, target), {}};
-    const bool copy = !loadable(w, ldw, T);
     const size_t piece = s.backward(copy);
     const uint32_t K64 = (uint32_t)s.K64, T64 = (uint32_t)s.T64;
     for (size_t v = 0; v < V; v += piece) {

@@ -4,7 +4,7 @@ import torch
 
 import loss_plain as plain
 import paper_1802_04434_amd as ss
-from test_gpu_loss import DEV, NAN, scratch_for
+from test_gpu_loss import DEV, NAN, both, check, scratch_for, sliced
 
 pytestmark = pytest.mark.gpu
 
@@ -42,3 +42,19 @@ def test_a_confident_rows_loss_does_not_go_by_the_size_of_its_logits(T, V, base)
     assert (off < 0.4 * base * base * 2 ** -24).all() or base < 100        # a step of lse would show
     assert ((loss.cpu().double() - want).abs() <= off).all(), float(((loss.cpu().double() - want).abs() / off).max())
     assert ((lse.cpu().double() - (base * base + want)).abs() <= off + plain.U32 * (base * base + want)).all()
+
+
+# several pieces of the vocabulary: of D, of copied weights, one that divides and one that does not; few rows, and many with a narrow head
+@pytest.mark.parametrize("T,V,K,pad", [(4096, 40_000, 64, 0), (4096, 40_000, 72, 3), (40, 30_003, 4096, 0), (40, 30_003, 4096, 1), (1, 20_000, 8200, 1), (2000, 70_001, 136, 8)])
+def test_pieces_stay_in_their_scratch(T, V, K, pad):
+    gen = torch.Generator(device=DEV).manual_seed(T + V + K + pad)
+    h = sliced(torch.randn(T, K, generator=gen, device=DEV).bfloat16(), pad, pad % 2)
+    w = sliced((torch.randn(V, K, generator=gen, device=DEV) * 2 / K ** 0.5).bfloat16(), pad, pad % 2)
+    target = torch.randint(0, V, (T,), generator=gen, device=DEV)
+    target[T // 2] = -1 if T > 1 else V - 1
+    dloss = torch.randn(T, generator=gen, device=DEV)
+    wanted = ss.new_cross_entropy_scratch(T, V, K).numel()
+    memory = torch.full((wanted + (1 << 20),), 0xA5, dtype=torch.uint8, device=DEV)
+    got = both(h, w, target, dloss, memory[:wanted])
+    assert (memory[wanted:] == 0xA5).all()
+    check(got, plain.softmax_loss(h, w, target, dloss), (target >= 0).cpu())
