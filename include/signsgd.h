@@ -455,7 +455,8 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
  * Softmax cross entropy of T rows h (T x K) against a head w (V x K), z = h w^T, without keeping z: the
  * last layer of a language model, whose logits would be its largest matrix.  h and w are bf16 (dt:
  * SS_BF16, else SS_ERR_DTYPE), products are exact, sums in fp32.
- *   h, w     in   a row every ldh / ldw elements, aligned to their element alone
+ *   h, w     in   a row every ldh / ldw elements (SS_LOSS_MAX_STRIDE at most, else SS_ERR_ARG), aligned
+ *                 to their element alone
  *   target   in   T int64 in DEVICE memory.  Below 0: the row has none; it adds nothing to any gradient,
  *                 whatever its entries of h are (infinities and NaN included).  V or more: the row's
  *                 loss, and with it the gradients, are NaN.
@@ -475,6 +476,7 @@ int ss_mx4_linear(const void *x, ss_dtype xdt, size_t T, size_t ldx, const uint8
 #define SS_LOSS_MAX_ROWS ((size_t)1 << 24)
 #define SS_LOSS_MAX_VOCAB ((size_t)1 << 24)
 #define SS_LOSS_MAX_WIDTH ((size_t)1 << 20)
+#define SS_LOSS_MAX_STRIDE ((size_t)1 << 21)
 #define SS_LOSS_MAX_ELEMENTS ((size_t)1 << 34)      /* of h, with T and K rounded up to 64 */
 size_t ss_cross_entropy_scratch_bytes(size_t T, size_t V, size_t K);
 
@@ -494,8 +496,9 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
  * bf16 on the way, relative to the largest |dloss| (2^-9 of an entry at most).
  *   lse      in   T x fp32, as ss_cross_entropy leaves it
  *   dloss    in   T x fp32: the weight of each row (1 / their number for a mean), NULL: 1
- *   dh, dw   out  T x K and V x K, bf16 or fp32, a row every lddh / lddw elements, aligned to
- *                 their element; either may be NULL: not wanted.
+ *   dh, dw   out  T x K and V x K, bf16 or fp32, a row every lddh / lddw elements, however many (rows
+ *                 of a larger gradient, such as every sequence's last token), aligned to their
+ *                 element; either may be NULL: not wanted.
  */
 int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V,
                           size_t K, size_t ldw, const int64_t *target, const float *lse,

@@ -360,7 +360,7 @@ def new_cross_entropy_scratch(rows, vocab, width, device="cuda"):
 
 def cross_entropy(h, w, target, loss, lse, scratch, stream=None):
     """ss_cross_entropy: lse[t] <- log sum_v exp(z[t, v]), loss[t] <- lse[t] - z[t, target[t]] with z = h w^T, which is not kept.
-    h: T x K and w: V x K, bfloat16, elements of a row side by side; target: T int64, below 0 where a row has none (loss 0);
+    h: T x K and w: V x K, bfloat16, elements of a row side by side, rows 2^21 elements apart at most; target: T int64, below 0 where a row has none (loss 0);
     loss, lse: T float32; scratch: new_cross_entropy_scratch(T, V, K)."""
     _check("ss_cross_entropy", (_marshal or _native()).cross_entropy(h, w, target, loss, lse, scratch, stream))
     return loss

@@ -24,7 +24,9 @@ inline Span matrix(const void *p, size_t rows, size_t cols, size_t ld, ss_dtype 
 inline bool bad_sizes(size_t T, size_t V, size_t K) {
     return T > SS_LOSS_MAX_ROWS || V > SS_LOSS_MAX_VOCAB || K == 0 || K > SS_LOSS_MAX_WIDTH || V == 0 || rounded(T, 64) * rounded(K, 64) > SS_LOSS_MAX_ELEMENTS;
 }
-inline bool bad_ld(size_t ld, size_t cols) { return ld < cols || ld > 2 * SS_LOSS_MAX_WIDTH; }
+// rows that are read, in place by offsets of 32 bits; and rows that are written, 2^40 elements of them, which no card holds
+inline bool bad_ld(size_t ld, size_t cols) { return ld < cols || ld > SS_LOSS_MAX_STRIDE; }
+inline bool bad_ld_out(size_t ld, size_t rows, size_t cols) { return ld < cols || (rows > 1 && ld > ((size_t)1 << 40) / (rows - 1)); }
 
 // Whether the products load the caller's matrix as it lies.  Rows at multiples of 16 bytes are; a load of 16 bytes also goes to multiples of 4, but takes longer, which many rows of h
 // repeat and a copy does not.  us, w as it lies / copied: a training pass of 2 rows against 19840 x 2258 134 / 171, of 1284 against 3350 x 1118 120 / 115.
@@ -183,7 +185,7 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
     int rc = check(h, dt, T, ldh, w, V, K, ldw, target);
     if (rc != SS_OK) return rc;
     if ((dhdt != SS_F32 && dhdt != SS_BF16) || (dwdt != SS_F32 && dwdt != SS_BF16)) return SS_ERR_DTYPE;
-    if ((dh && bad_ld(lddh, K)) || (dw && bad_ld(lddw, K))) return SS_ERR_ARG;
+    if ((dh && bad_ld_out(lddh, T, K)) || (dw && bad_ld_out(lddw, V, K))) return SS_ERR_ARG;
     if (T == 0 && !dw) return SS_OK;
     if (T && (!lse || !scratch || (!dh && !dw))) return SS_ERR_NULL;
     if (!element_aligned(lse, SS_F32) || !element_aligned(dloss, SS_F32) || !element_aligned(dh, dhdt) || !element_aligned(dw, dwdt) || !aligned16(scratch)) return SS_ERR_ALIGN;

@@ -775,6 +775,8 @@ struct Head {
         if (h.dtype != SS_BF16) raise_type("h", -1, "must be bfloat16");
         if (w.dtype != SS_BF16) raise_type("w", -1, "must be bfloat16");
         if (w.cols != h.cols) raise_type("w", -1, "must have h's %zu columns, got %zu", h.cols, w.cols);
+        for (const Matrix *x : {&h, &w})
+            if (x->ld > SS_LOSS_MAX_STRIDE) raise_type(x == &h ? "h" : "w", -1, "must have its rows %zu elements apart at most, got %zu", SS_LOSS_MAX_STRIDE, x->ld);
         target = (const int64_t *)rows(a[2], kI64, "target");
         same_device(a[1], device, "w");
     }

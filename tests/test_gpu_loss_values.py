@@ -4,7 +4,7 @@ import torch
 
 import loss_plain as plain
 import paper_1802_04434_amd as ss
-from test_gpu_loss import DEV, NAN, both, check, scratch_for, sliced
+from test_gpu_loss import DEV, NAN, both, case, check, scratch_for, sliced
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,40 @@ def test_pieces_stay_in_their_scratch(T, V, K, pad):
     got = both(h, w, target, dloss, memory[:wanted])
     assert (memory[wanted:] == 0xA5).all()
     check(got, plain.softmax_loss(h, w, target, dloss), (target >= 0).cpu())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradients_into_rows_far_apart(dtype):
+    """of every sequence's last token, and of a head whose rows lie in a larger buffer: beyond 2^21 elements, in all beyond 4 GiB"""
+    T, V, K, length, width = 19, 300, 200, 1024, 4096
+    h, w, target, dloss = (x.to(DEV) for x in case(T, V, K))
+    scratch = scratch_for(T, V, K)
+    want = both(h, w, target, dloss, scratch, dtype, dtype)
+    hidden = torch.full((T, length, width), NAN, dtype=dtype, device=DEV)
+    dh = hidden[:, -1, 4:4 + K]
+    rows = torch.full((V * ((1 << 23) + 5),), NAN, dtype=dtype, device=DEV)
+    dw = rows.as_strided((V, K), ((1 << 23) + 5, 1))
+    assert dh.stride(0) == 1 << 22 and dw.stride(0) * V * dw.element_size() > 1 << 32
+    ss.cross_entropy_grad(h, w, target, want["lse"], dloss, dh, dw, scratch)
+    assert torch.equal(dh, want["dh"]) and torch.equal(dw, want["dw"])
+    assert torch.isnan(hidden[:, :-1]).all() and torch.isnan(hidden[:, -1, :4]).all() and torch.isnan(hidden[:, -1, 4 + K:]).all()
+    for at in (0, 1, V - 1):        # around a row nothing is written
+        assert torch.isnan(rows[at * dw.stride(0) + K:(at + 1) * dw.stride(0)]).all()
+
+
+def test_rows_too_far_apart_to_be_read_are_refused_by_name():
+    T, V, K = 3, 20, 64
+    h, w, target, dloss = (x.to(DEV) for x in case(T, V, K))
+    loss, lse, scratch = torch.empty(T, device=DEV), torch.empty(T, device=DEV), scratch_for(T, V, K)
+    buffer = torch.zeros(V * ((1 << 21) + 1), dtype=torch.bfloat16, device=DEV)
+    apart = lambda x, n: buffer.as_strided(x.shape, (n, 1)).copy_(x)  # noqa: E731
+    for name, tensors in (("h", (apart(h, (1 << 21) + 1), w)), ("w", (h, apart(w, (1 << 21) + 1)))):
+        for call in (lambda: ss.cross_entropy(*tensors, target, loss, lse, scratch), lambda: ss.cross_entropy_grad(*tensors, target, lse, dloss, torch.empty_like(h), torch.empty_like(w), scratch)):
+            with pytest.raises(TypeError, match="%s must have its rows 2097152 elements apart at most, got 2097153" % name):
+                call()
+    # at the limit, in place and copied
+    want = both(h, w, target, dloss, scratch)
+    for offset in (0, 1):
+        at = buffer[offset:].as_strided(w.shape, (1 << 21, 1), offset).copy_(w)
+        got = both(h, at, target, dloss, scratch)
+        assert all(torch.equal(got[name], want[name]) for name in want)
