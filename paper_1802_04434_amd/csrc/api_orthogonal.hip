@@ -21,8 +21,11 @@ struct Stack {
         return count > SS_ORTHOGONAL_MAX_COUNT || rows > SS_ORTHOGONAL_MAX_DIM || cols > SS_ORTHOGONAL_MAX_DIM || std::min(rows, cols) > SS_ORTHOGONAL_MAX_SHORT ||
                (!empty() && rounded(rows, 64) * rounded(cols, 64) > SS_ORTHOGONAL_MAX_ELEMENTS / count);
     }
-    // matrices in rows `ld` apart, `apart` elements from one to the next
-    bool bad(size_t ld, size_t apart) const { return ld < cols || ld > ((size_t)1 << 40) || (count > 1 && apart < (rows - 1) * ld + cols) || apart > ((size_t)1 << 48); }
+    // matrices in rows `ld` apart, `apart` elements from one to the next; together 2^41 elements, which no card holds, so that no span of theirs passes 64 bits
+    bool bad(size_t ld, size_t apart) const {
+        constexpr size_t kMost = (size_t)1 << 40;
+        return ld < cols || (rows > 1 && ld > kMost / (rows - 1)) || (count > 1 && (apart < (rows - 1) * ld + cols || apart > kMost / (count - 1)));
+    }
     Span of(const void *p, size_t ld, size_t apart, ss_dtype dt, bool written) const { return span(p, ((count - 1) * apart + (rows - 1) * ld + cols) * grad_bytes(dt), written); }
 };
 

@@ -35,7 +35,20 @@ def check_rows_that_are_written(c):
     assert c.grad(5, 6, 64, lddh=1 << 30, dh=good, h=good + (1 << 32)) == (ARG, [])
 
 
-CHECKS = {f.__name__: f for f in (check_rows_that_are_read, check_rows_that_are_written)}
+def check_matrices(c):
+    good = c.buffer(1 << 50)
+    for call, name in ((c.orthogonalize, "out"), (c.step, "x")):
+        assert call(3, 5, 6, ld=1 << 36, apart=1 << 39, g=good)[0] == OK
+        # 2^14 + 1 matrices 2^48 elements apart: their last byte is 2^64 + 4 from the first, which a sum of 64 bits takes for 4
+        for count, ld, apart in (((1 << 14) + 1, 1, 1 << 48), (3, 1, (1 << 39) + 1), (3, 1, 1 << 62), (3, 1, (1 << 64) - 1)):
+            assert call(count, 1, 1, ld=ld, apart=apart, g=good, **{name: good + (1 << 30)}) == (ARG, []), (count, apart)
+        for ld in ((1 << 40) // 4 + 1, 1 << 61, (1 << 64) - 1):
+            assert call(1, 5, 6, ld=ld, apart=0, g=good) == (ARG, []), ld
+        assert call(1, 1, 6, ld=1 << 61, apart=1 << 61, g=good)[0] == OK           # one row of one matrix has no distance
+        assert call(3, 5, 6, ld=1 << 30, apart=1 << 34, g=good, **{name: good + (1 << 33)}) == (ARG, [])
+
+
+CHECKS = {f.__name__: f for f in (check_rows_that_are_read, check_rows_that_are_written, check_matrices)}
 
 
 @pytest.mark.parametrize("name", sorted(CHECKS))
