@@ -254,6 +254,12 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
     };
     f32x16 c[T][T] = {};
     // b's k beyond the last one, which a's zeros alone would not undo: they may be NaN
+    auto mask_of = [&](int j, int left) {       // left: k that this lane has, of 32
+        u32x4 mask;
+#pragma unroll
+        for (int d = 0; d < 4; ++d) mask[d] = 8 * j + 2 * d + 1 < left ? ~0u : 8 * j + 2 * d < left ? 0xFFFFu : 0u;
+        return mask;
+    };
     u32x4 kept[4];
     auto keep = [&](Fragments<T> &f, int j) {
         if constexpr (End::kRagged)
@@ -262,12 +268,7 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
     };
     auto mask = [&] {
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j)
-#pragma unroll
-            for (uint32_t d = 0; d < 4; ++d) {
-                const uint32_t k = 32 * q + 8 * j + 2 * d;
-                kept[j][d] = k + 1 < p.tail ? ~0u : k < p.tail ? 0xFFFFu : 0u;
-            }
+        for (int j = 0; j < 4; ++j) kept[j] = mask_of(j, (int)p.tail - 32 * (int)q);
     };
     if constexpr (End::kRagged)
 #pragma unroll
@@ -280,19 +281,29 @@ __global__ __launch_bounds__(256, 1) void tiles_kernel(const TilesArgs<typename 
             for (int i = 0; i < L; ++i) wa.fetch(lds, i, 0, coming.step, coming.a, wave), wb.fetch(lds, i, kUnit, coming.step, coming.b, wave);
             arrived<0>();
             __builtin_amdgcn_s_barrier();
-            Fragments<T> f[4];
+            // Where the last step is not whole, two quarters at a time, with masks that are made right where they are used: all four at once, or masks kept through the steps, take more than 64
+            // registers, and four blocks share a compute unit, not eight.  us so / with 116 registers: gradients of 1000 rows against 50000 x 33 90 / 101, 900 against 32000 x 250 95 / 106, 64 against 84096 x 212 52.5 / 53.8.
+            constexpr int kAtOnce = End::kRagged ? 2 : 4;
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j0 = 0; j0 < 4; j0 += kAtOnce) {
+                Fragments<T> f[kAtOnce];
 #pragma unroll
-                for (int i = 0; i < 2 * T; ++i) read(f[j], i, j, 0, kUnit);
-            if constexpr (End::kRagged) {
-                if (step + 1 == to) mask();
-            }
+                for (int j = 0; j < kAtOnce; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                keep(f[j], j);
+                    for (int i = 0; i < 2 * T; ++i) read(f[j], i, j0 + j, 0, kUnit);
+                if constexpr (End::kRagged) {
+                    if (step + 1 == to) {
+                        int left = (int)p.tail - 32 * (int)q;
+                        asm volatile("" : "+v"(left));
 #pragma unroll
-                for (int part = 0; part < 2 * T; ++part) multiply<E>(c, f[j], part);
+                        for (int j = 0; j < kAtOnce; ++j) f[j].b[0] &= mask_of(j0 + j, left);
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+                    for (int part = 0; part < 2 * T; ++part) multiply<E>(c, f[j], part);
+                if constexpr (End::kRagged) __builtin_amdgcn_sched_barrier(0);
             }
             arrived<0>();
         }
