@@ -95,3 +95,28 @@ def test_rows_too_far_apart_to_be_read_are_refused_by_name():
         at = buffer[offset:].as_strided(w.shape, (1 << 21, 1), offset).copy_(w)
         got = both(h, at, target, dloss, scratch)
         assert all(torch.equal(got[name], want[name]) for name in want)
+
+
+# few rows against many tokens, and many rows, whose D comes in two pieces of the vocabulary
+LIKELY = [(1, 70_001, 64), (2, 30_003, 200), (2000, 70_001, 136), (70, 9001, 520)]
+
+
+def likely_tokens(T, V, K):
+    """h, w, target, dloss, and the tokens that have all of the probability but a hundredth, each about as much as the others: the last nine, and some on both sides of tiles and pieces"""
+    gen = torch.Generator().manual_seed(T + V + K)
+    pieces = -(-V // ((1 << 27) // (-(-T // 64) * 64) // 256 * 256))
+    edge = -(-V // pieces // 256) * 256 if pieces > 1 else 4096
+    hot = torch.tensor([0, 63, 64, 255, 256, edge - 1, edge, *range(V - 9, V)])
+    h, w = torch.randn(T, K, generator=gen) / (4 * K ** 0.5), torch.randn(V, K, generator=gen)
+    h[:, 0], w[:, 0] = 16, 0
+    w[hot, 0] = 1                                    # e^16 times as likely: 8.9e6 to 70001 times at most e^(1/2)
+    target = torch.randint(1, 60, (T,), generator=gen)
+    return h.bfloat16(), w.bfloat16(), target, torch.rand(T, generator=gen) + 0.5, hot
+
+
+@pytest.mark.parametrize("T,V,K", LIKELY)
+def test_no_likely_token_is_left_out_of_a_gradient(T, V, K):
+    h, w, target, dloss, _ = (x.to(DEV) for x in likely_tokens(T, V, K))
+    for pad in (0, 1):
+        got = both(sliced(h, pad, pad), sliced(w, pad, pad), target, dloss, scratch_for(T, V, K), torch.float32, torch.float32)
+        check(got, plain.softmax_loss(h, w, target, dloss))
