@@ -42,27 +42,40 @@ struct StatsEnd {
     }
     template <int T, bool INSIDE>
     static __device__ __forceinline__ void rows(const Args &a, const f32x16 (&c)[T][T], uint32_t m, uint32_t n, uint32_t part, uint32_t M, uint32_t N, uint32_t r, uint32_t q) {
-        const uint32_t left = N > n + 4 * q ? N - n - 4 * q : 0;      // columns from this lane's first one on: a part of none counts for nothing
+        uint32_t left = N > n + 4 * q ? N - n - 4 * q : 0;      // columns from this lane's first one on: a part of none counts for nothing
+        // 16 T comparisons with it kept for their next use take two scalar registers each, more than there are
+        auto compare_anew = [&] {
+            if constexpr (!INSIDE) asm volatile("" : "+v"(left));
+        };
 #pragma unroll
         for (int i = 0; i < T; ++i) {
+            // Read from the matrix unit's registers row by row: the compiler would bring all 16 T^2 at once, 40 of them for T = 4 by way of memory (700 MB with 8192 rows against 128000).
+            f32x16 z[T];
+#pragma unroll
+            for (int k = 0; k < T; ++k) {
+                z[k] = c[i][k];
+                asm volatile("" : "+a"(z[k]));
+            }
             const uint32_t row = m + i * 32 + r;
             const bool there = row < M;
             const int64_t target = there ? a.target[row] : -1;
             float top = -__builtin_inff();
+            compare_anew();
 #pragma unroll
             for (int k = 0; k < T; ++k)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (INSIDE || k * 32 + e / 4 * 8 + e % 4 < left) top = fmaxf(top, c[i][k][e]);
+                    if (INSIDE || k * 32 + e / 4 * 8 + e % 4 < left) top = fmaxf(top, z[k][e]);
             top = fmaxf(top, __shfl_xor(top, 32));
             // NaN passes: it is not the largest, but its exponential is NaN.  Where there is none but -infinity their exponentials are 0.
             const float from = top == -__builtin_inff() ? 0.0f : top;
             float sum = 0;
+            compare_anew();
 #pragma unroll
             for (int k = 0; k < T; ++k)
 #pragma unroll
                 for (int e = 0; e < 16; ++e)
-                    if (INSIDE || k * 32 + e / 4 * 8 + e % 4 < left) sum += exp_of(c[i][k][e] - from);
+                    if (INSIDE || k * 32 + e / 4 * 8 + e % 4 < left) sum += exp_of(z[k][e] - from);
             sum += __shfl_xor(sum, 32);
             if (there && q == 0) a.parts[(size_t)(a.part0 + part) * M + row] = Part{top, sum};
             const int64_t hit = target < 0 ? -1 : target - a.first - n - 4 * q;
@@ -71,7 +84,7 @@ struct StatsEnd {
                 for (int k = 0; k < T; ++k)
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
-                        if ((uint32_t)hit == k * 32 + e / 4 * 8 + e % 4) a.picked[row] = c[i][k][e];
+                        if ((uint32_t)hit == k * 32 + e / 4 * 8 + e % 4) a.picked[row] = z[k][e];
             }
         }
     }

@@ -48,3 +48,8 @@ def test_kernels_of_a_few_steps_leave_room_for_eight_blocks(kernels):
     assert ends == {"SoftmaxEndILb0", "SoftmaxEndILb1", "GradientEnd", "SquareEnd", "PolynomialEnd", "UpdateEnd"}, ends
     for name, k in short.items():
         assert k["vgpr_count"] <= 64 and k["vgpr_spill_count"] == 0 and 8 * k["group_segment_fixed_size"] <= 160 << 10, (name, k)
+
+
+def test_no_product_keeps_sums_in_memory(kernels):
+    tiles = {n: k for n, k in kernels.items() if "tiles_kernel" in n}
+    assert len(tiles) > 20 and not [n for n, k in tiles.items() if k["vgpr_spill_count"]]
