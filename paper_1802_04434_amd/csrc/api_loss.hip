@@ -59,7 +59,8 @@ constexpr size_t kForwardEntries = (size_t)1 << 36, kLeastRoom = (size_t)1 << 27
 struct Sizes {
     size_t T, V, K, T64, K64, room;
     Sizes(size_t t, size_t v, size_t k) : T(t), V(v), K(k), T64(rounded(t, 64)), K64(rounded(k, 64)), room(std::min(std::max(T64 * V / 2, kLeastRoom), kMostRoom)) {}
-    // tokens of a piece, where each takes `each` entries: all pieces but the last alike, and that no shorter than it has to be
+    // tokens of a piece, where each takes `each` entries: all alike but for the last, which is hardly shorter.  us of the gradients so / as many as there is room for, and the rest: 4096 rows
+    // against 32000 x 2048 with copied weights 1,488 / 1,580, 8192 against 128000 x 512 3,760 / 4,010, but 8192 against 128000 x 4096 19,980 / 19,830.
     size_t piece(size_t entries, size_t each) const {
         const size_t most = std::max(entries / each / kEdge * kEdge, 4 * kEdge), pieces = (V + most - 1) / most;
         return std::min(rounded((V + pieces - 1) / pieces, kEdge), V);
