@@ -483,8 +483,9 @@ size_t ss_cross_entropy_scratch_bytes(size_t T, size_t V, size_t K);
 /*
  * lse_t <- log sum_v exp(z_tv);  loss_t <- lse_t - z_t,target_t, 0 in rows without a target.  The loss
  * is computed from the largest logit: a likely target's is not rounded by the size of the logits.
- *   loss, lse  out  T x fp32.  A row with an infinite or NaN logit has NaN, but one of -infinity
- *                   next to finite ones counts as zero probability.
+ *   loss, lse  out  T x fp32.  A row with a NaN or a logit of +infinity has NaN.  A logit of -infinity
+ *                   next to finite ones counts as zero probability (the loss of such a target is
+ *                   +infinity); where all are, lse is -infinity and the loss NaN.
  */
 int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V,
                      size_t K, size_t ldw, const int64_t *target, float *loss, float *lse,
@@ -493,7 +494,7 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
 /*
  * With D_tv = dloss_t (exp(z_tv - lse_t) - [v = target_t]), 0 in rows without a target:
  * dh <- D w, dw <- D^T h, sums in fp32, rounded once to the gradient's type.  D is rounded to
- * bf16 on the way, relative to the largest |dloss| (2^-9 of an entry at most).
+ * bf16 on the way, relative to the largest |dloss| (2^-8 of an entry at most).
  *   lse      in   T x fp32, as ss_cross_entropy leaves it
  *   dloss    in   T x fp32: the weight of each row (1 / their number for a mean), NULL: 1
  *   dh, dw   out  T x K and V x K, bf16 or fp32, a row every lddh / lddw elements, however many (rows
@@ -516,10 +517,14 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
  * norm to between 0.68 and 1.2).  A matrix of zeros gives zeros; one with an infinity or a NaN, NaN everywhere.
  * The scale of g makes no difference.  Products take operands of 11 bits, X is held in 22 and sums in fp32: five steps are off by
  * 1e-3 to 2e-3 of the result's norm, which is what rounding it to bf16 costs; further steps enlarge that.
+ * An fp32 result with a shorter side below 1024, whose last steps multiply 22 bits, is off by 1e-4 to 1e-3;
+ * with a shorter side of 128 at most by 1e-7 to 1e-5, as long as the matrix, or the stack of them, is not so
+ * large that it is worked on as larger ones are.
  *   count, rows, cols   a stack of matrices, each by itself; any may be 0
  *   ld, apart           elements from one row to the next, and from one matrix to the next
  *   scratch             ss_orthogonalize_scratch_bytes(count, rows, cols) bytes, under the same terms
- *                       as that of ss_cross_entropy
+ *                       as that of ss_cross_entropy; wanted of every call, also for matrices so small
+ *                       that it stays untouched
  */
 #define SS_ORTHOGONAL_MAX_COUNT ((size_t)65535)
 #define SS_ORTHOGONAL_MAX_DIM ((size_t)1 << 20)

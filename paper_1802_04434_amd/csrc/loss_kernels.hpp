@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256) void join_stats_kernel(const JoinArgs a) {
 
 // D of a row t is scale x factor_t x (softmax - target).  scale is the largest |dloss| of a row with a target and is multiplied in when the
 // gradients are whole: where all rows weigh the same the factors are 1, and the target's entries, softmax - 1, lose next to nothing to
-// bf16, where dloss itself would be off by up to 2^-9 in all rows alike.
+// bf16, where dloss itself would be off by up to 2^-8 in all rows alike.
 struct FactorArgs {
     const float *dloss;            // NULL: 1
     const int64_t *target;

@@ -120,3 +120,20 @@ def test_no_likely_token_is_left_out_of_a_gradient(T, V, K):
     for pad in (0, 1):
         got = both(sliced(h, pad, pad), sliced(w, pad, pad), target, dloss, scratch_for(T, V, K), torch.float32, torch.float32)
         check(got, plain.softmax_loss(h, w, target, dloss))
+
+
+def test_logits_of_minus_infinity():
+    """beside finite ones: probability zero, and an infinite loss where it is the target's; nothing else in a row: lse is -infinity, the loss no number, and 0 where there is no target"""
+    T, V, K = 66, 200, 64
+    h, w, target, _ = case(T, V, K, masked=0)
+    h[:, 0], w[:, 0] = 1, float("-inf")
+    h[3, 1:] = 0
+    target[3], target[5], target[7] = 4, -1, 150
+    loss, lse = torch.empty(T, device=DEV), torch.empty(T, device=DEV)
+    ss.cross_entropy(h.to(DEV), w.to(DEV), target.to(DEV), loss, lse, scratch_for(T, V, K))
+    there = (target >= 0).to(DEV)
+    assert (lse == float("-inf")).all() and torch.isnan(loss[there]).all() and loss[5] == 0
+    w[4, 0] = 2                                            # all but one token
+    ss.cross_entropy(h.to(DEV), w.to(DEV), target.to(DEV), loss, lse, scratch_for(T, V, K))
+    hit = (target == 4).to(DEV)
+    assert torch.isfinite(lse).all() and lse[3] == 2 and (loss[hit] == 0).all() and loss[5] == 0 and (loss[there & ~hit] == float("inf")).all()
