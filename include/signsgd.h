@@ -497,9 +497,9 @@ int ss_cross_entropy(const void *h, ss_dtype dt, size_t T, size_t ldh, const voi
  * bf16 on the way, relative to the largest |dloss| (2^-8 of an entry at most).
  *   lse      in   T x fp32, as ss_cross_entropy leaves it
  *   dloss    in   T x fp32: the weight of each row (1 / their number for a mean), NULL: 1
- *   dh, dw   out  T x K and V x K, bf16 or fp32, a row every lddh / lddw elements, however many (rows
- *                 of a larger gradient, such as every sequence's last token), aligned to their
- *                 element; either may be NULL: not wanted.
+ *   dh, dw   out  T x K and V x K, bf16 or fp32, a row every lddh / lddw elements (also more than
+ *                 SS_LOSS_MAX_STRIDE: rows of a larger gradient, such as every sequence's last token;
+ *                 2^40 in all), aligned to their element; either may be NULL: not wanted.
  */
 int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, const void *w, size_t V,
                           size_t K, size_t ldw, const int64_t *target, const float *lse,
@@ -521,7 +521,8 @@ int ss_cross_entropy_grad(const void *h, ss_dtype dt, size_t T, size_t ldh, cons
  * with a shorter side of 128 at most by 1e-7 to 1e-5, as long as the matrix, or the stack of them, is not so
  * large that it is worked on as larger ones are.
  *   count, rows, cols   a stack of matrices, each by itself; any may be 0
- *   ld, apart           elements from one row to the next, and from one matrix to the next
+ *   ld, apart           elements from one row to the next, and from one matrix to the next; rows, and
+ *                       matrices, are 2^40 in all apart at most (SS_ERR_ARG)
  *   scratch             ss_orthogonalize_scratch_bytes(count, rows, cols) bytes, under the same terms
  *                       as that of ss_cross_entropy; wanted of every call, also for matrices so small
  *                       that it stays untouched
